@@ -334,6 +334,72 @@ int rabitq_scan(rabitq_index_t index, const rabitq_query_repr* repr, const float
 int rabitq_merge(rabitq_index_t index, const uint64_t* cand_keys, const int32_t* cand_cnt, int64_t nq, int32_t k,
                  int32_t nprobe, int64_t* out_ids, float* out_dists, void* stream);
 
+/* ---- Products by list, and products of 8-bit integers ----
+ * A batch whose pairs rabitq_build_probe_lists has regrouped can be multiplied by a matrix that belongs to the list of each
+ * pair (a learned map for every list; the experts of a layer whose router is the coarse probe), forward and backward, and rows
+ * can be held as int8 codes with a scale each, multiplied by int8 rows as integers.  The calls need no handle: every
+ * buffer is the caller's, in the memory of the current HIP device; they only enqueue kernels on `stream`, allocate nothing and
+ * may be captured into a HIP graph.  Two calls may overlap in time if neither writes what the other reads or writes.
+ * Matrices are row-major with a row stride ("ld...", in elements, at least the row's length); any stride and any alignment of
+ * the element type is taken, rows that start at multiples of 16 bytes are the fast case.  Outputs must not overlap inputs.
+ * Sums are fp32 (int32 for codes) and are taken in an order that depends on the sizes only: equal calls give equal bits. */
+typedef enum { RABITQ_F32 = 0, RABITQ_F16 = 1, RABITQ_BF16 = 2 } rabitq_dtype;
+
+/* The pairs of a batch, regrouped by list.  List g holds the positions pair_off[g] .. pair_off[g+1) and its matrix W[g]
+ * is [n][k]; position i stands for pair p = pair_ids[i], which belongs to row p / nprobe of the inputs x.  pair_off and pair_ids
+ * are those of rabitq_build_probe_lists; rows that were sorted by list beforehand need no pair_ids (position i is pair i).
+ * Offsets are taken as if they lay in [0, pairs], and a position whose pair id lies outside [0, pairs) is passed over.  A pair may be
+ * named once: of a pair named more often, one of the results is written (and its gradient is one of the
+ * terms).  Positions outside every list take part in nothing. */
+typedef struct {
+  int32_t groups;          /* lists, >= 1                                              */
+  int32_t nprobe;          /* pairs per row of x, >= 1                                 */
+  int64_t pairs;           /* rows of x times nprobe, 0 .. 2^31 - 1                    */
+  int32_t n, k;            /* rows and columns of each list's matrix, 1 .. 2^20        */
+  const int32_t* pair_off; /* device, [groups+1]                                       */
+  const int32_t* pair_ids; /* device, [pairs], or NULL                                 */
+} rabitq_lists;
+
+/* out[p] = W[list of p] x[p / nprobe] for every pair named: out [pairs][n], x [pairs / nprobe][k], W [groups][n][k] with
+ * stride_w elements from one matrix to the next (at least (n - 1) ldw + k), all of type `dtype`; one rounding, of the fp32 sum.
+ * Rows of pairs that no list names are left as they were.
+ * Errors (all calls of this section): RABITQ_EINVAL (null pointer, size or stride out of range, unknown type, more than
+ * 2^23 tiles of work), RABITQ_EHIP. */
+int rabitq_grouped_matmul(const rabitq_lists* lists, int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                          int64_t stride_w, void* out, int64_t ldo, void* stream);
+
+/* Gradient of x: dx[q] = sum over the pairs p of row q that a list names, in ascending p, of W[list of p]^T dout[p]
+ * (fp32 sum, rounded once).  dx [pairs / nprobe][k], dout [pairs][n].  A row none of whose pairs is named is left as it was.
+ * scratch: device, rabitq_grouped_dx_scratch_bytes(lists) bytes at a multiple of 16 (0 bytes, and NULL, for nprobe 1). */
+int64_t rabitq_grouped_dx_scratch_bytes(const rabitq_lists* lists);
+int rabitq_grouped_matmul_dx(const rabitq_lists* lists, int32_t dtype, const void* dout, int64_t ldd, const void* w,
+                             int64_t ldw, int64_t stride_w, void* dx, int64_t ldx, void* scratch, void* stream);
+
+/* Gradient of the matrices: dw[g] = sum over the positions of list g of dout[p] x[p / nprobe]^T, [groups][n][k] (fp32
+ * sum, rounded once); zeros for a list without pairs.  Every element of dw is written.
+ * scratch: device, rabitq_grouped_dw_scratch_bytes(lists) bytes at a multiple of 16 (may be 0, then NULL is taken). */
+int64_t rabitq_grouped_dw_scratch_bytes(const rabitq_lists* lists);
+int rabitq_grouped_matmul_dw(const rabitq_lists* lists, int32_t dtype, const void* dout, int64_t ldd, const void* x,
+                             int64_t ldx, void* dw, int64_t ldw, int64_t stride_w, void* scratch, void* stream);
+
+/* Rows of numbers as int8: scale[i] = the fp32 number nearest to max_j |x[i][j]| / 127 (1 if that is 0), codes[i][j] = the
+ * whole number nearest to x[i][j] / scale[i], ties to the even one, -127 .. 127.  A row that holds an infinity or a NaN
+ * gets scale NaN and codes 0, so that what is computed from it shows it.  k: 1 .. 2^20. */
+int rabitq_quantize_rows(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int32_t k, int8_t* codes, int64_t ldc,
+                         float* scale, void* stream);
+
+/* out[i][j] = scale_a[i] scale_b[j] sum_t a[i][t] b[j][t]: a [m][k] and b [n][k] int8 (any codes, -128 among them), the
+ * sum exact in int32 (k <= 131071), converted to fp32, times scale_a, times scale_b, and rounded to out_dtype.
+ * a: queries or tokens with their scales; b: stored vectors, or the rows (output channels) of a layer's matrix. */
+int rabitq_matmul_i8(const int8_t* a, int64_t lda, const float* scale_a, const int8_t* b, int64_t ldb, const float* scale_b,
+                     int64_t m, int64_t n, int32_t k, void* out, int32_t out_dtype, int64_t ldo, void* stream);
+
+/* rabitq_grouped_matmul on codes: out[p][j] = scale_x[p / nprobe] scale_w[g][j] sum_t x[p / nprobe][t] w[g][j][t], with
+ * scale_w [groups][n]; k <= 131071. */
+int rabitq_grouped_matmul_i8(const rabitq_lists* lists, const int8_t* x, int64_t ldx, const float* scale_x, const int8_t* w,
+                             int64_t ldw, int64_t stride_w, const float* scale_w, void* out, int32_t out_dtype, int64_t ldo,
+                             void* stream);
+
 /* Text of the last error raised on the calling thread ("" if none). */
 const char* rabitq_last_error(void);
 

@@ -1,0 +1,86 @@
+// Products by list and products of 8-bit integers: what the launchers take, and how a kernel finds its rows.
+#pragma once
+#include "rq_device.h"
+
+namespace rq {
+
+constexpr int DTYPE_I8 = 3;  // operands only; behind the rabitq_dtype values
+constexpr int64_t MAX_TILES = 1 << 23;  // workgroups of a launch: times 512 threads, what a grid may hold
+inline int64_t dtype_bytes(int dtype) { return dtype == RABITQ_F32 ? 4 : dtype == DTYPE_I8 ? 1 : 2; }
+
+// One product, whichever direction.  `a` has a row per pair or per row of x, `b` is the matrices (forward and dx) or x (dw).
+struct ProductArgs {
+  const void* a;
+  const void* b;
+  void* out;
+  int64_t lda, ldb, ldo;
+  int64_t stride;             // between the matrices of two lists, in b or (dw) in out
+  const float* scale_a;       // codes only: one per row of a, one per row of b ([groups][n])
+  const float* scale_b;
+  const int32_t* pair_off;    // null: one list of all positions
+  const int32_t* pair_ids;    // null: position i is pair i
+  int64_t pairs;
+  int64_t n;
+  int k, groups, nprobe;
+  int out_dtype;
+  uint8_t* named;             // dx of several probes: set to 1 for every pair a list names, or null
+};
+
+// Positions of a list, within 0 .. pairs whatever the offsets hold.
+struct Span {
+  int64_t begin, end;
+};
+__device__ __forceinline__ int64_t clamp_off(const ProductArgs& p, int g) {
+  const int64_t o = p.pair_off[g];
+  return o < 0 ? 0 : o > p.pairs ? p.pairs : o;
+}
+__device__ __forceinline__ Span span_of(const ProductArgs& p, int g) {
+  if (p.pair_off == nullptr) return Span{0, p.pairs};
+  return Span{clamp_off(p, g), clamp_off(p, g + 1)};
+}
+// The pair at a position, or -1.
+__device__ __forceinline__ int64_t pair_at(const ProductArgs& p, int64_t pos) {
+  if (p.pair_ids == nullptr) return pos;
+  const int64_t i = p.pair_ids[pos];
+  return (uint64_t)i < (uint64_t)p.pairs ? i : -1;
+}
+
+// Tiles of `rows` positions are numbered so that list g owns those from F(g) = off[g] / rows + g on: F grows by at least the
+// ceil(length / rows) tiles that the list needs, so no table of tiles has to be made, pairs / rows + groups tiles are enough, and
+// the list of a tile is the last g with F(g) <= tile.  Searched 64 ways at a time, one offset per lane (a level reads one line or
+// 64 scattered words; 2 levels to 4096 lists).
+__device__ __forceinline__ int list_of_tile(const ProductArgs& p, int64_t tile, int rows, int lane) {
+  int lo = 0, len = p.groups;  // the answer lies in lo .. lo + len - 1
+  while (len > 1) {
+    const int step = (len + 63) / 64;
+    const int g = lo + lane * step;
+    const bool below = lane * step < len && clamp_off(p, g) / rows + g <= tile;
+    const int c = __popcll(__ballot(below));  // F ascends, so these are the first c lanes (at least one if lo holds)
+    const int at = c > 0 ? (c - 1) * step : 0;
+    lo += at;
+    len = min(step, len - at);
+  }
+  return lo;
+}
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(_Float16 v) { return (float)v; }
+__device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
+
+__device__ __forceinline__ void store_as(void* out, int dtype, int64_t at, float v) {
+  if (dtype == RABITQ_F32) static_cast<float*>(out)[at] = v;
+  else if (dtype == RABITQ_F16) static_cast<_Float16*>(out)[at] = (_Float16)v;
+  else static_cast<__bf16*>(out)[at] = (__bf16)v;
+}
+
+// dtype: of the operands.  All sizes and pointers checked by the caller, work to do.
+int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st);
+int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st);
+int launch_product_dw(const ProductArgs& p, int dtype, hipStream_t st);
+int launch_clear_bytes(void* at, int64_t n, hipStream_t st);
+int launch_sum_named(const float* parts, const uint8_t* named, int64_t rows, int nprobe, int k, void* out, int dtype, int64_t ldo,
+                     hipStream_t st);
+int launch_quantize_rows(const void* x, int dtype, int64_t ldx, int64_t rows, int k, int8_t* codes, int64_t ldc, float* scale,
+                         hipStream_t st);
+
+}  // namespace rq

@@ -25,7 +25,9 @@ EXPORTS = [
     "rabitq_index_upload", "rabitq_index_build", "rabitq_index_export", "rabitq_index_free", "rabitq_search", "rabitq_search_noalloc", "rabitq_set_option", "rabitq_index_info",
     "rabitq_stage_ms", "rabitq_rotate", "rabitq_query_prep", "rabitq_qhat_stride", "rabitq_coarse_probe",
     "rabitq_probe_list_scratch_words", "rabitq_probe_select_variant", "rabitq_cand_capacity", "rabitq_build_probe_lists", "rabitq_seed_threshold", "rabitq_scan",
-    "rabitq_merge", "rabitq_last_error",
+    "rabitq_merge", "rabitq_grouped_matmul", "rabitq_grouped_dx_scratch_bytes", "rabitq_grouped_matmul_dx",
+    "rabitq_grouped_dw_scratch_bytes", "rabitq_grouped_matmul_dw", "rabitq_quantize_rows", "rabitq_matmul_i8",
+    "rabitq_grouped_matmul_i8", "rabitq_last_error",
 ]
 
 
@@ -50,6 +52,11 @@ class _BuildParams(C.Structure):
     _fields_ = [("dim", C.c_int32), ("nlist", C.c_int32), ("n", C.c_int64), ("total_bits", C.c_int32),
                 ("metric", C.c_int32), ("kmeans_iters", C.c_int32), ("train_size", C.c_int64),
                 ("epsilon0", C.c_float), ("rotation", C.c_void_p), ("center", C.c_int32)]
+
+
+class _Lists(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("nprobe", C.c_int32), ("pairs", C.c_int64), ("n", C.c_int32), ("k", C.c_int32),
+                ("pair_off", C.c_void_p), ("pair_ids", C.c_void_p)]
 
 
 _lib = None
@@ -92,9 +99,19 @@ def load_library() -> C.CDLL:
     lib.rabitq_seed_threshold.argtypes = [vp, C.POINTER(_QueryRepr), vp, vp, vp, i64, i32, i32, vp, vp]
     lib.rabitq_scan.argtypes = [vp, C.POINTER(_QueryRepr), vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, vp]
     lib.rabitq_merge.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp]
+    lists = C.POINTER(_Lists)
+    lib.rabitq_grouped_matmul.argtypes = [lists, i32, vp, i64, vp, i64, i64, vp, i64, vp]
+    lib.rabitq_grouped_matmul_dx.argtypes = [lists, i32, vp, i64, vp, i64, i64, vp, i64, vp, vp]
+    lib.rabitq_grouped_matmul_dw.argtypes = [lists, i32, vp, i64, vp, i64, vp, i64, i64, vp, vp]
+    for name in ("rabitq_grouped_dx_scratch_bytes", "rabitq_grouped_dw_scratch_bytes"):
+        getattr(lib, name).argtypes = [lists]
+        getattr(lib, name).restype = i64
+    lib.rabitq_quantize_rows.argtypes = [vp, i32, i64, i64, i32, vp, i64, vp, vp]
+    lib.rabitq_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, i64, i64, i32, vp, i32, i64, vp]
+    lib.rabitq_grouped_matmul_i8.argtypes = [lists, vp, i64, vp, vp, i64, i64, vp, vp, i32, i64, vp]
     for name in EXPORTS:
         if name not in ("rabitq_last_error", "rabitq_index_info", "rabitq_probe_list_scratch_words",
-                        "rabitq_cand_capacity", "rabitq_qhat_stride", "rabitq_probe_select_variant"):
+                        "rabitq_grouped_dx_scratch_bytes", "rabitq_grouped_dw_scratch_bytes", "rabitq_cand_capacity", "rabitq_qhat_stride", "rabitq_probe_select_variant"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -351,6 +368,178 @@ class Index:
         _check(load_library().rabitq_merge(self._h, _dev(cand_keys, torch.int64), _dev(cand_cnt, torch.int32), nq, k,
                                            nprobe, out_ids.data_ptr(), out_d.data_ptr(), _stream()))
         return out_ids, out_d
+
+
+# ---- products by list and products of 8-bit integers -------------------------------
+# Plain calls on tensors of the current device: strided rows are taken as they are, nothing is copied, and no gradient is
+# recorded (grouped_matmul_dx and grouped_matmul_dw are the backward pass).
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _here(t: torch.Tensor, dtype, dims: int, what: str):
+    """A tensor of the current device with `dims` dimensions, whose last one is contiguous and whose rows do not overlap."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise RabitqError(f"{what}: expected a tensor on the current CUDA device")
+    if t.dtype != dtype or t.dim() != dims:
+        raise RabitqError(f"{what}: expected {dims} dimensions of {dtype}, got {t.dim()} of {t.dtype}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise RabitqError(f"{what} requires a gradient, which this call does not record: pass it detached or under "
+                          "torch.no_grad()")
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise RabitqError(f"{what}: the last dimension must be contiguous")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    """The row stride; of a single row, whose stride says nothing, the row's length."""
+    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _matrix_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else _ld(t) * t.shape[1]
+
+
+def _float_type(t: torch.Tensor, what: str):
+    if not isinstance(t, torch.Tensor) or t.dtype not in DTYPES:
+        raise RabitqError(f"{what}: expected float32, float16 or bfloat16")
+    return t.dtype
+
+
+def _output(out, shape, dtype, device, what="out"):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(_here(out, dtype, len(shape), what).shape) != tuple(shape):
+        raise RabitqError(f"{what}: expected the shape {tuple(shape)}, got {tuple(out.shape)}")
+    return out
+
+
+def _lists_of(groups: int, n: int, k: int, pairs: int, nprobe: int, pair_off, pair_ids) -> "_Lists":
+    _here(pair_off, torch.int32, 1, "pair_off")
+    if pair_off.shape[0] != groups + 1:
+        raise RabitqError(f"pair_off must hold {groups + 1} offsets, got {pair_off.shape[0]}")
+    if pair_ids is not None and _here(pair_ids, torch.int32, 1, "pair_ids").shape[0] != pairs:
+        raise RabitqError(f"pair_ids must hold {pairs} pairs, got {pair_ids.shape[0]}")
+    return _Lists(groups, nprobe, pairs, n, k, pair_off.data_ptr(), None if pair_ids is None else pair_ids.data_ptr())
+
+
+def _nprobe(nprobe) -> int:
+    if int(nprobe) != nprobe or not 1 <= nprobe <= 0x7fffffff:
+        raise RabitqError("nprobe must be a whole number from 1 on")
+    return int(nprobe)
+
+
+def _scales(t, shape, what):
+    if tuple(_here(t, torch.float32, len(shape), what).shape) != tuple(shape) or not t.is_contiguous():
+        raise RabitqError(f"{what}: expected a contiguous tensor of the shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _scratch(n: int, device):
+    if n < 0:
+        _check(int(n))
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def grouped_matmul(x, w, pair_off, pair_ids=None, nprobe: int = 1, out=None):
+    """rabitq_grouped_matmul: out[p] = w[list of p] @ x[p // nprobe] for the pairs of pair_off / pair_ids
+    (Index.build_probe_lists).  x [nq, k] and w [lists, n, k] of float32, float16 or bfloat16; returns out [nq * nprobe, n].
+    Rows of pairs that no list names are left as they were (in a new output: undefined)."""
+    dt = _float_type(x, "x")
+    _here(x, dt, 2, "x"), _here(w, dt, 3, "w")
+    (nq, k), (g, n, _), nprobe = x.shape, w.shape, _nprobe(nprobe)
+    if w.shape[2] != k:
+        raise RabitqError(f"rows of x have {k} elements, those of w {w.shape[2]}")
+    ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids)
+    out = _output(out, (nq * nprobe, n), dt, x.device)
+    _check(load_library().rabitq_grouped_matmul(C.byref(ls), DTYPES[dt], x.data_ptr(), _ld(x), w.data_ptr(), _ld(w),
+                                                _matrix_stride(w), out.data_ptr(), _ld(out), _stream()))
+    return out
+
+
+def grouped_matmul_dx(dout, w, pair_off, pair_ids=None, nprobe: int = 1, out=None):
+    """rabitq_grouped_matmul_dx: the gradient of grouped_matmul with respect to x, [nq, k], from dout [nq * nprobe, n]; the
+    sum over a row's nprobe pairs is in it.  Rows none of whose pairs a list names are left as they were."""
+    dt, nprobe = _float_type(dout, "dout"), _nprobe(nprobe)
+    _here(dout, dt, 2, "dout"), _here(w, dt, 3, "w")
+    pairs, (g, n, k) = dout.shape[0], w.shape
+    if dout.shape[1] != n:
+        raise RabitqError(f"rows of dout have {dout.shape[1]} elements, matrices of w {n} rows")
+    if pairs % nprobe:
+        raise RabitqError("dout must have nprobe rows per row of x")
+    ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids)
+    out = _output(out, (pairs // nprobe, k), dt, dout.device)
+    lib = load_library()
+    scratch = _scratch(lib.rabitq_grouped_dx_scratch_bytes(C.byref(ls)), dout.device)
+    _check(lib.rabitq_grouped_matmul_dx(C.byref(ls), DTYPES[dt], dout.data_ptr(), _ld(dout), w.data_ptr(), _ld(w),
+                                        _matrix_stride(w), out.data_ptr(), _ld(out),
+                                        None if scratch is None else scratch.data_ptr(), _stream()))
+    return out
+
+
+def grouped_matmul_dw(dout, x, pair_off, pair_ids=None, nprobe: int = 1, out=None):
+    """rabitq_grouped_matmul_dw: the gradient of grouped_matmul with respect to w, [lists, n, k], from dout [nq * nprobe, n]
+    and x [nq, k].  Zeros for lists without pairs."""
+    dt, nprobe = _float_type(dout, "dout"), _nprobe(nprobe)
+    _here(dout, dt, 2, "dout"), _here(x, dt, 2, "x")
+    (pairs, n), (nq, k) = dout.shape, x.shape
+    if pairs != nq * nprobe:
+        raise RabitqError(f"dout must have {nq * nprobe} rows, got {pairs}")
+    _here(pair_off, torch.int32, 1, "pair_off")
+    g = pair_off.shape[0] - 1
+    ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids)
+    out = _output(out, (g, n, k), dt, dout.device)
+    lib = load_library()
+    scratch = _scratch(lib.rabitq_grouped_dw_scratch_bytes(C.byref(ls)), dout.device)
+    _check(lib.rabitq_grouped_matmul_dw(C.byref(ls), DTYPES[dt], dout.data_ptr(), _ld(dout), x.data_ptr(), _ld(x),
+                                        out.data_ptr(), _ld(out), _matrix_stride(out),
+                                        None if scratch is None else scratch.data_ptr(), _stream()))
+    return out
+
+
+def quantize_rows(x, codes=None, scale=None):
+    """rabitq_quantize_rows: x [rows, k] of float32, float16 or bfloat16 -> int8 codes [rows, k] and float32 scale [rows], with
+    x about codes * scale[:, None]."""
+    dt = _float_type(x, "x")
+    _here(x, dt, 2, "x")
+    rows, k = x.shape
+    codes = _output(codes, (rows, k), torch.int8, x.device, "codes")
+    scale = _output(scale, (rows,), torch.float32, x.device, "scale")
+    _check(load_library().rabitq_quantize_rows(x.data_ptr(), DTYPES[dt], _ld(x), rows, k, codes.data_ptr(), _ld(codes),
+                                               _scales(scale, (rows,), "scale"), _stream()))
+    return codes, scale
+
+
+def matmul_i8(a, scale_a, b, scale_b, out_dtype=torch.float32, out=None):
+    """rabitq_matmul_i8: out[i, j] = scale_a[i] * scale_b[j] * sum_t a[i, t] * b[j, t] for int8 a [m, k] and b [n, k]."""
+    _here(a, torch.int8, 2, "a"), _here(b, torch.int8, 2, "b")
+    (m, k), n = a.shape, b.shape[0]
+    if b.shape[1] != k:
+        raise RabitqError(f"rows of a have {k} elements, those of b {b.shape[1]}")
+    if out_dtype not in DTYPES:
+        raise RabitqError("out_dtype must be float32, float16 or bfloat16")
+    out = _output(out, (m, n), out_dtype, a.device)
+    _check(load_library().rabitq_matmul_i8(a.data_ptr(), _ld(a), _scales(scale_a, (m,), "scale_a"), b.data_ptr(), _ld(b),
+                                           _scales(scale_b, (n,), "scale_b"), m, n, k, out.data_ptr(), DTYPES[out_dtype],
+                                           _ld(out), _stream()))
+    return out
+
+
+def grouped_matmul_i8(x, scale_x, w, scale_w, pair_off, pair_ids=None, nprobe: int = 1, out_dtype=torch.float32, out=None):
+    """rabitq_grouped_matmul_i8: grouped_matmul on codes, x [nq, k] with scale_x [nq] and w [lists, n, k] with scale_w
+    [lists, n]."""
+    _here(x, torch.int8, 2, "x"), _here(w, torch.int8, 3, "w")
+    (nq, k), (g, n, _), nprobe = x.shape, w.shape, _nprobe(nprobe)
+    if w.shape[2] != k:
+        raise RabitqError(f"rows of x have {k} elements, those of w {w.shape[2]}")
+    if out_dtype not in DTYPES:
+        raise RabitqError("out_dtype must be float32, float16 or bfloat16")
+    ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids)
+    out = _output(out, (nq * nprobe, n), out_dtype, x.device)
+    _check(load_library().rabitq_grouped_matmul_i8(
+        C.byref(ls), x.data_ptr(), _ld(x), _scales(scale_x, (nq,), "scale_x"), w.data_ptr(), _ld(w), _matrix_stride(w),
+        _scales(scale_w, (g, n), "scale_w"), out.data_ptr(), DTYPES[out_dtype], _ld(out), _stream()))
+    return out
 
 
 def index_from_arrays(meta: dict, dev: dict) -> Index:
