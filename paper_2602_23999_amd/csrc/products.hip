@@ -1,97 +1,7 @@
 // Products by list (forward, gradient of the inputs, gradient of the matrices) and products of int8 codes with scales.
-#include "rq_products.h"
+#include "rq_product_tile.h"
 
 namespace rq {
-
-constexpr int TB = 64, KB = 16;  // tile of the output, contraction per step
-
-enum { FORWARD = 0, GRAD_X = 1, GRAD_W = 2 };
-
-template <class T>
-struct AccOf { using type = float; };
-template <>
-struct AccOf<int8_t> { using type = int; };
-__device__ __forceinline__ float operand(float v) { return v; }
-__device__ __forceinline__ float operand(_Float16 v) { return (float)v; }
-__device__ __forceinline__ float operand(__bf16 v) { return (float)v; }
-__device__ __forceinline__ int operand(int8_t v) { return v; }
-
-template <class T, int OP>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs p) {
-  using Acc = typename AccOf<T>::type;
-  __shared__ Acc As[KB][TB + 1], Bs[KB][TB + 1];
-  __shared__ int64_t row_a[TB], row_out[TB];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const T* a = static_cast<const T*>(p.a);
-  const T* b = static_cast<const T*>(p.b);
-  int g;
-  Span s;
-  const int jt = (int)(((OP == FORWARD ? p.n : p.k) + TB - 1) / TB);
-  const int64_t tile = blockIdx.x / jt;
-  int64_t i0, j0 = (int64_t)(blockIdx.x % jt) * TB, ni, nj, nc;
-  if (OP == GRAD_W) {
-    const int64_t it = (p.n + TB - 1) / TB;
-    g = (int)(tile / it);
-    s = span_of(p, g);
-    i0 = tile % it * TB;
-    ni = p.n; nj = p.k; nc = s.end - s.begin;
-  } else {
-    g = p.pair_off ? list_of_tile(p, tile, TB, lane) : 0;
-    s = span_of(p, g);
-    const int64_t first = p.pair_off ? s.begin / TB + g : 0;
-    i0 = s.begin + (tile - first) * TB;
-    if (i0 < s.begin || i0 >= s.end) return;
-    ni = s.end; nj = OP == FORWARD ? p.n : p.k; nc = OP == FORWARD ? p.k : p.n;
-    for (int i = tid; i < TB; i += 256) {
-      const int64_t pr = i0 + i < s.end ? pair_at(p, i0 + i) : -1;
-      row_out[i] = pr;
-      row_a[i] = pr < 0 ? -1 : OP == FORWARD ? pr / p.nprobe : pr;
-    }
-    __syncthreads();
-    b += (int64_t)g * p.stride;
-  }
-  Acc acc[4][4] = {};
-  const int ti = tid / 16, tj = tid % 16;
-  for (int64_t c0 = 0; c0 < nc; c0 += KB) {
-    for (int e = tid; e < TB * KB; e += 256) {
-      if (OP == GRAD_W) {
-        const int i = e % TB, c = e / TB;
-        const int64_t pr = c0 + c < nc ? pair_at(p, s.begin + c0 + c) : -1;
-        As[c][i] = pr >= 0 && i0 + i < ni ? operand(a[pr * p.lda + i0 + i]) : Acc(0);
-        Bs[c][i] = pr >= 0 && j0 + i < nj ? operand(b[pr / p.nprobe * p.ldb + j0 + i]) : Acc(0);
-      } else {
-        const int c = e % KB, i = e / KB;
-        As[c][i] = c0 + c < nc && row_a[i] >= 0 ? operand(a[row_a[i] * p.lda + c0 + c]) : Acc(0);
-        if (OP == FORWARD) {
-          Bs[c][i] = c0 + c < nc && j0 + i < nj ? operand(b[(j0 + i) * p.ldb + c0 + c]) : Acc(0);
-        } else {
-          const int j = e % TB, cc = e / TB;
-          Bs[cc][j] = c0 + cc < nc && j0 + j < nj ? operand(b[(c0 + cc) * p.ldb + j0 + j]) : Acc(0);
-        }
-      }
-    }
-    __syncthreads();
-    for (int c = 0; c < KB; ++c)
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[u][v] += As[c][ti * 4 + u] * Bs[c][tj + 16 * v];
-    __syncthreads();
-  }
-  for (int u = 0; u < 4; ++u) {
-    const int i = ti * 4 + u;
-    const int64_t ro = OP == GRAD_W ? (i0 + i < ni ? i0 + i : -1) : row_out[i];
-    if (ro < 0) continue;
-    if (OP == GRAD_X && p.named && j0 == 0 && tj == 0) p.named[ro] = 1;
-    for (int v = 0; v < 4; ++v) {
-      const int64_t j = j0 + tj + 16 * v;
-      if (j >= nj) continue;
-      float r = (float)acc[u][v];
-      if (sizeof(T) == 1) r = r * p.scale_a[row_a[i]] * p.scale_b[(int64_t)g * p.n + j];
-      store_as(p.out, p.out_dtype, (OP == GRAD_W ? (int64_t)g * p.stride : 0) + ro * p.ldo + j, r);
-    }
-  }
-}
 
 __global__ __launch_bounds__(256) void clear_bytes_kernel(uint8_t* at, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) at[i] = 0;
@@ -136,34 +46,57 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
   }
 }
 
-template <int OP>
-static int launch_op(const ProductArgs& p, int dtype, int64_t tiles, hipStream_t st) {
-  if (tiles > MAX_TILES) {
+static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
+
+template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
+static int launch_tiles(ProductArgs p, hipStream_t st) {
+  const int64_t width = OP == FORWARD ? p.n : p.k;
+  p.tiles = up(width, BJ) * (OP == GRAD_W ? up(p.n, BI) * p.groups : p.pairs / BI + p.groups);
+  if (p.tiles > MAX_TILES) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
-  const unsigned grid = (unsigned)tiles;
-  switch (dtype) {
-    case RABITQ_F32: product_kernel<float, OP><<<grid, 256, 0, st>>>(p); break;
-    case RABITQ_F16: product_kernel<_Float16, OP><<<grid, 256, 0, st>>>(p); break;
-    case RABITQ_BF16: product_kernel<__bf16, OP><<<grid, 256, 0, st>>>(p); break;
-    default: if constexpr (OP == FORWARD) product_kernel<int8_t, OP><<<grid, 256, 0, st>>>(p);
-  }
+  const size_t lds = 2 * (BI + BJ) * 128 + BI * sizeof(int);
+  auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, FAST>;
+  static const hipError_t granted =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  RQ_HIP(granted);
+  kernel<<<(unsigned)(up(p.tiles, 8) * 8), 64 * WI * WJ, lds, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }
 
-static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
+// Rows of whole 16-byte pieces at multiples of 16 bytes: the pieces can go to LDS without registers.
+static bool fast_rows(const ProductArgs& p, int op, int dtype) {
+  const int64_t sz = dtype_bytes(dtype), per = 16 / sz;
+  const int64_t in_a = op == FORWARD ? p.k : p.n;  // elements of a row of each operand
+  return in_a % per == 0 && p.k % per == 0 && p.lda % per == 0 && p.ldb % per == 0 && (op == GRAD_W || p.stride % per == 0 || p.groups == 1) &&
+         reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && reinterpret_cast<uintptr_t>(p.b) % 16 == 0;
+}
 
-int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st) {
-  return launch_op<FORWARD>(p, dtype, (p.pairs / TB + p.groups) * up(p.n, TB), st);
+template <class T, int OP>
+static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
+  if (!fast_rows(p, OP, dtype)) return launch_tiles<T, OP, 128, 128, 2, 2, false>(p, st);
+  const int64_t width = OP == FORWARD ? p.n : p.k;
+  const int64_t big = up(width, 256) * (OP == GRAD_W ? up(p.n, 256) * p.groups : p.pairs / 256 + p.groups);
+  if (big >= 512) return launch_tiles<T, OP, 256, 256, 2, 4, true>(p, st);
+  return launch_tiles<T, OP, 128, 128, 2, 2, true>(p, st);
 }
-int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st) {
-  return launch_op<GRAD_X>(p, dtype, (p.pairs / TB + p.groups) * up(p.k, TB), st);
+
+template <int OP>
+static int launch_op(const ProductArgs& p, int dtype, hipStream_t st) {
+  switch (dtype) {
+    case RABITQ_F32: return launch_typed<float, OP>(p, dtype, st);
+    case RABITQ_F16: return launch_typed<_Float16, OP>(p, dtype, st);
+    case RABITQ_BF16: return launch_typed<__bf16, OP>(p, dtype, st);
+  }
+  if constexpr (OP == FORWARD) return launch_typed<int8_t, OP>(p, dtype, st);
+  return RABITQ_EINVAL;
 }
-int launch_product_dw(const ProductArgs& p, int dtype, hipStream_t st) {
-  return launch_op<GRAD_W>(p, dtype, up(p.n, TB) * up(p.k, TB) * p.groups, st);
-}
+
+int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<FORWARD>(p, dtype, st); }
+int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<GRAD_X>(p, dtype, st); }
+int launch_product_dw(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<GRAD_W>(p, dtype, st); }
 
 int launch_clear_bytes(void* at, int64_t n, hipStream_t st) {
   clear_bytes_kernel<<<(unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, st>>>(static_cast<uint8_t*>(at), n);

@@ -23,6 +23,7 @@ struct ProductArgs {
   int64_t n;
   int k, groups, nprobe;
   int out_dtype;
+  int64_t tiles;              // of the launch
   uint8_t* named;             // dx of several probes: set to 1 for every pair a list names, or null
 };
 
