@@ -51,8 +51,10 @@ static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
 static int launch_tiles(ProductArgs p, hipStream_t st) {
   const int64_t width = OP == FORWARD ? p.n : p.k;
-  p.tiles = up(width, BJ) * (OP == GRAD_W ? up(p.n, BI) * p.groups : p.pairs / BI + p.groups);
-  if (p.tiles > MAX_TILES) {
+  p.chunk = std::max<int64_t>(1, up(width, BJ) / 8);
+  p.tiles = up(width, BJ) * (OP == GRAD_W ? up(p.n, BI) * p.groups : p.pair_off ? p.pairs / BI + p.groups : up(p.pairs, BI));
+  const int64_t grid = up(p.tiles, 8 * p.chunk) * 8 * p.chunk;
+  if (grid > MAX_GRID / (64 * WI * WJ)) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
@@ -61,7 +63,7 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
   static const hipError_t granted =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   RQ_HIP(granted);
-  kernel<<<(unsigned)(up(p.tiles, 8) * 8), 64 * WI * WJ, lds, st>>>(p);
+  kernel<<<(unsigned)grid, 64 * WI * WJ, lds, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }

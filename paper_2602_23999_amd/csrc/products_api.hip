@@ -47,7 +47,7 @@ int check_lists(const char* call, const rabitq_lists* l) {
 ProductArgs args_of(const rabitq_lists* l) {
   ProductArgs p{};
   p.pair_off = l->pair_off; p.pair_ids = l->pair_ids; p.pairs = l->pairs; p.n = l->n; p.k = l->k;
-  p.groups = l->groups; p.nprobe = l->nprobe;
+  p.groups = l->groups; p.probe = divisor(l->nprobe);
   return p;
 }
 
@@ -162,7 +162,7 @@ int rabitq_matmul_i8(const int8_t* a, int64_t lda, const float* scale_a, const i
     if (!aligned(scale_a, 4) || !aligned(scale_b, 4) || !aligned(out, dtype_bytes(out_dtype))) return bad(call, "pointer not aligned to its type");
     ProductArgs p{};
     p.a = a; p.lda = lda; p.b = b; p.ldb = ldb; p.scale_a = scale_a; p.scale_b = scale_b;
-    p.pairs = m; p.n = n; p.k = k; p.groups = 1; p.nprobe = 1; p.out = out; p.ldo = ldo; p.out_dtype = out_dtype;
+    p.pairs = m; p.n = n; p.k = k; p.groups = 1; p.probe = divisor(1); p.out = out; p.ldo = ldo; p.out_dtype = out_dtype;
     return launch_product_forward(p, DTYPE_I8, (hipStream_t)stream);
   });
 }

@@ -6,65 +6,82 @@
 // bytes per row and step; one whose i or j runs along memory (the matrix of dx, both operands of dw) as lines of c, and is
 // turned on the way to the registers.  Either way a step takes 128 bytes of every row: 128 codes, 64 halves or 32 floats.
 #pragma once
+#include <type_traits>
+
 #include "rq_products.h"
 
 namespace rq {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 enum ProductOp { FORWARD = 0, GRAD_X = 1, GRAD_W = 2 };
 
-// 16 bytes of an operand per lane: row (column) lane % 16, the (lane / 16)-th quarter of 64 bytes along c.
+// 32 x 32 products of 32 bytes along c (a quarter of a step).  An operand is 16 bytes per lane: its row (column) is lane % 32, its
+// half of the 32 bytes lane / 32.  PARTS instructions take them (f32: one for each of the four elements of every lane).
 template <class T>
-struct Mma {  // f32: the four instructions take elements 0, 1, 2, 3 of every lane's quarter
-  using Acc = f32x4;
-  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) {
-    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
-    return c;
+struct Mma {
+  using Acc = f32x16;
+  static constexpr int PARTS = 4;
+  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c, int part) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(f32x4, a)[part], __builtin_bit_cast(f32x4, b)[part], c, 0, 0, 0);
   }
 };
 template <>
 struct Mma<_Float16> {
-  using Acc = f32x4;
-  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  using Acc = f32x16;
+  static constexpr int PARTS = 1;
+  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c, int) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
 };
 template <>
 struct Mma<__bf16> {
-  using Acc = f32x4;
-  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  using Acc = f32x16;
+  static constexpr int PARTS = 1;
+  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c, int) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
 };
 template <>
 struct Mma<int8_t> {
-  using Acc = i32x4;
-  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+  using Acc = i32x16;
+  static constexpr int PARTS = 1;
+  static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c, int) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
+
+// Register r of lane l of an accumulator is row 8 (r / 4) + 4 (l / 32) + r % 4 of the first operand, column l % 32 of the second.  The
+// first operand holds j, in an order that leaves a lane 16 neighbouring columns of the output: its row m is j = j_of_row(m).
+__device__ __forceinline__ int j_of_row(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
 // 16 bytes per lane from memory to LDS without registers: lane l's go to lds + 16 l.  Not waited for by the compiler: the kernel
 // waits for all of them in front of the barrier behind which they are read.
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
+// (As builtins and not in the asm, so that the compiler's own count of LDS reads in flight starts again from none.)
 __device__ __forceinline__ void wait_and_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
-// Where the lines' 16-byte pieces lie, so that the lanes of a read spread over the banks.
-__device__ __forceinline__ int swizzle_i(int row) { return row & 7; }
-__device__ __forceinline__ int swizzle_j(int row) { return (row & 3) | ((row >> 1) & 4); }
+// Where the lines' 16-byte pieces lie, so that the lanes of a read spread over the 64 banks.  A read of 16 bytes per lane takes 16
+// lanes at a time, of which no two are alike in bits 0 to 3 (0 .. 15 as well as 0 .. 3, 12 .. 15, 20 .. 27): bit 0 picks the half of
+// the banks that an odd or even line starts at, bits 1 to 3 the place of the piece.  Turned operands are read 64 (f32: 128) bytes of 4
+// (2) lines at a time.
+__device__ __forceinline__ int swizzle_i(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int swizzle_j(int row) { return ((row >> 1) & 1) | ((row >> 3) & 2) | (row & 4); }  // of m, row = j_of_row(m)
 template <int SIZE>
 __device__ __forceinline__ int swizzle_turned(int c, int piece) {  // of a line of one c
-  if constexpr (SIZE == 4) return piece ^ (((c >> 2) & 3) << 2);
-  else return piece ^ (((c & 3) | ((c >> 1) & 4)) << 1);
+  if constexpr (SIZE == 4) return piece ^ (((c >> 2) & 1) << 3);
+  else return piece ^ ((c & 3) << 2);
 }
 
 // 16 bytes of which the first `valid` elements exist, the others zero; any alignment.
@@ -92,7 +109,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   constexpr int NT = 64 * WI * WJ, SZ = sizeof(T), EPC = 16 / SZ, STEP = 128 / SZ;
   constexpr bool TA = OP == GRAD_W, TB = OP != FORWARD;
   constexpr int NA = BI * 8 / NT, NB = BJ * 8 / NT;       // pieces per thread and step
-  constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;     // 16 x 16 products per wavefront
+  constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;     // 32 x 32 products per wavefront
   constexpr int STAGE = (BI + BJ) * 128;
   using Acc = typename Mma<T>::Acc;
   extern __shared__ __align__(16) char smem[];
@@ -104,27 +121,31 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   const int nj = OP == FORWARD ? (int)0 : p.k;
   const int64_t width = OP == FORWARD ? p.n : (int64_t)nj;  // of the output
   const int64_t jt = (width + BJ - 1) / BJ;
-  const int64_t per = (gridDim.x + 7) / 8;
-  const int64_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);  // consecutive tiles on one XCD
+  // Workgroups go to the 8 XCDs in turn; each XCD gets `chunk` neighbouring tiles of every 8 chunk, an eighth of the columns where
+  // there are that many: its share of b stays in its own L2 while the rows pass by, and no XCD gets more than a chunk of the work more
+  // than another.
+  const int64_t turn = blockIdx.x >> 3;
+  const int64_t id = (turn / p.chunk * 8 + (blockIdx.x & 7)) * p.chunk + turn % p.chunk;
   if (id >= p.tiles) return;
   const int64_t tile = id / jt, j0 = id % jt * BJ;
   int g;
   Span s;
-  int64_t i0, iend, nc;
+  int64_t i0, iend;
+  uint32_t nc;  // length of the contraction, below 2^31: positions and pairs are 32-bit numbers
   if constexpr (OP == GRAD_W) {
     const int64_t it = (p.n + BI - 1) / BI;
     g = (int)(tile / it);
     s = span_of(p, g);
     i0 = tile % it * BI;
     iend = p.n;
-    nc = s.end > s.begin ? s.end - s.begin : 0;
+    nc = s.end > s.begin ? (uint32_t)(s.end - s.begin) : 0;
   } else {
     g = p.pair_off ? list_of_tile(p, tile, BI, lane) : 0;
     s = span_of(p, g);
     i0 = s.begin + (tile - (p.pair_off ? s.begin / BI + g : 0)) * BI;
     iend = s.end;
     if (i0 < s.begin || i0 >= iend) return;
-    nc = OP == FORWARD ? p.k : p.n;
+    nc = OP == FORWARD ? p.k : (uint32_t)p.n;
     for (int i = tid; i < BI; i += NT) row_pair[i] = i0 + i < iend ? (int)pair_at(p, i0 + i) : -1;
     __syncthreads();
   }
@@ -132,108 +153,83 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   const char* b = static_cast<const char*>(p.b) + (OP == GRAD_W ? 0 : (int64_t)g * p.stride * SZ);
   const char* zeros = reinterpret_cast<const char*>(product_zeros);
 
+  const int jleft = (int)(width - j0 < BJ ? width - j0 : BJ);  // columns of the tile that exist
   // this thread's pieces of a step: where they start, and which c (or, of turned operands, which i or j) they hold
-  const char *pa[NA], *pb[NB];
+  const char* pa[NA];
   const int line = tid >> 3;
-  const int ca = ((tid & 7) ^ swizzle_i(line)) * EPC, cb = ((tid & 7) ^ swizzle_j(line)) * EPC;  // (the same for all q)
+  const uint32_t ca = ((tid & 7) ^ swizzle_i(line)) * EPC, cb = ((tid & 7) ^ swizzle_j(line)) * EPC;  // (the same for all q)
   constexpr int PA = BI * SZ / 16, PB = BJ * SZ / 16;     // pieces of a line of a turned operand
   if constexpr (!TA) {
 #pragma unroll
     for (int q = 0; q < NA; ++q) {
       const int pr = row_pair[line + q * (NT / 8)];
-      const int64_t row = pr < 0 ? 0 : OP == FORWARD ? pr / p.nprobe : pr;  // (a row that is not there reads row 0, unused)
+      const int64_t row = pr < 0 ? 0 : OP == FORWARD ? p.probe.of(pr) : pr;  // (a row that is not there reads row 0, unused)
       pa[q] = a + (row * p.lda + ca) * SZ;
     }
   }
-  if constexpr (!TB) {
-#pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      const int64_t row = j0 + line + q * (NT / 8);
-      pb[q] = b + ((row < width ? row : 0) * p.ldb + cb) * SZ;
-    }
-  } else if constexpr (OP == GRAD_X) {
-#pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      const int c = (tid + q * NT) / PB, piece = swizzle_turned<SZ>(c, (tid + q * NT) % PB);
-      pb[q] = b + (c * p.ldb + j0 + piece * EPC) * SZ;
-    }
-  }
-  // dw: the pairs of this thread's lines, a step ahead
-  constexpr int LA = TA ? NA : 1, LB = TA ? NB : 1;
-  int pair_a[LA], pair_b[LB];
-  auto find_pairs = [&](int64_t c0) {
-    if constexpr (OP == GRAD_W) {
+  const char* pb = nullptr;  // piece 0; the others lie whole lines behind it
+  if constexpr (!TB) pb = b + ((j0 + line) * p.ldb + cb) * SZ;
+  if constexpr (OP == GRAD_X) pb = b + (tid / PB * p.ldb + j0) * SZ;
+  // dw: the pairs of this thread's lines, a step ahead (the lines of both operands are the same)
+  constexpr int LP = TA ? NA : 1;
+  static_assert(!TA || BI == BJ);
+  int pairs_next[LP];
+  auto find_pairs = [&](uint32_t c0) {
+    if constexpr (TA) {
 #pragma unroll
       for (int q = 0; q < NA; ++q) {
-        const int64_t c = c0 + (tid + q * NT) / PA;
-        pair_a[q] = c < nc ? (int)pair_at(p, s.begin + c) : -1;
-      }
-#pragma unroll
-      for (int q = 0; q < NB; ++q) {
-        const int64_t c = c0 + (tid + q * NT) / PB;
-        pair_b[q] = c < nc ? (int)pair_at(p, s.begin + c) : -1;
+        const uint32_t c = c0 + (uint32_t)(tid + q * NT) / PA;
+        pairs_next[q] = c < nc ? (int)pair_at(p, s.begin + c) : -1;
       }
     }
   };
-  // where piece q of the step at c0 lies, and how many of its elements exist
-  auto piece_a = [&](int q, int64_t c0, const char*& from) -> int64_t {
+  // where piece q of the step at c0 lies, and how many of its elements exist (none or more than there are, as may be)
+  auto piece_a = [&](int q, uint32_t c0, const char*& from) -> int {
     if constexpr (!TA) {
-      from = pa[q];
-      pa[q] += 128;
-      return nc - c0 - ca;
+      from = pa[q] + (uint64_t)c0 * SZ;
+      return c0 + ca < nc ? (int)(nc - c0 - ca) : 0;
     } else {
       const int col = swizzle_turned<SZ>((tid + q * NT) / PA, (tid + q * NT) % PA) * EPC;
-      from = a + ((int64_t)pair_a[q] * p.lda + i0 + col) * SZ;
-      return pair_a[q] < 0 ? 0 : iend - i0 - col;
+      from = a + ((int64_t)pairs_next[q] * p.lda + i0 + col) * SZ;
+      return pairs_next[q] < 0 ? 0 : (int)(iend - i0) - col;
     }
   };
-  auto piece_b = [&](int q, int64_t c0, const char*& from) -> int64_t {
+  auto piece_b = [&](int q, uint32_t c0, const char*& from) -> int {
     if constexpr (!TB) {
-      from = pb[q];
-      pb[q] += 128;
-      return nc - c0 - cb;
+      from = pb + ((int64_t)(q * (NT / 8)) * p.ldb + c0) * SZ;
+      return line + q * (NT / 8) < jleft && c0 + cb < nc ? (int)(nc - c0 - cb) : 0;
     } else if constexpr (OP == GRAD_X) {
       const int c = (tid + q * NT) / PB, piece = swizzle_turned<SZ>(c, (tid + q * NT) % PB);
-      from = pb[q];
-      pb[q] += STEP * p.ldb * SZ;
-      return c0 + c < nc ? width - j0 - piece * EPC : 0;
+      from = pb + ((int64_t)(c0 + q * (NT / PB)) * p.ldb + piece * EPC) * SZ;
+      return c0 + c < nc ? jleft - piece * EPC : 0;
     } else {
       const int col = swizzle_turned<SZ>((tid + q * NT) / PB, (tid + q * NT) % PB) * EPC;
-      from = b + ((int64_t)(pair_b[q] / p.nprobe) * p.ldb + j0 + col) * SZ;
-      return pair_b[q] < 0 ? 0 : width - j0 - col;
+      from = b + ((int64_t)p.probe.of(pairs_next[q]) * p.ldb + j0 + col) * SZ;
+      return pairs_next[q] < 0 ? 0 : jleft - col;
     }
   };
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  auto fetch = [&](int64_t c0, int buf) {  // straight to LDS
-    const uint32_t at = lds + buf * STAGE + wave * 1024;
-#pragma unroll
-    for (int q = 0; q < NA; ++q) {
-      const char* from;
-      const int64_t valid = piece_a(q, c0, from);
-      load_to_lds(valid > 0 ? from : zeros, at + q * (NT * 16));
-    }
-#pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      const char* from;
-      const int64_t valid = piece_b(q, c0, from);
-      load_to_lds(valid > 0 ? from : zeros, at + BI * 128 + q * (NT * 16));
-    }
+  auto fetch_piece = [&](int q, uint32_t c0, int buf) {  // straight to LDS
+    const uint32_t at = lds + buf * STAGE + wave * 1024 + (q < NA ? q * (NT * 16) : BI * 128 + (q - NA) * (NT * 16));
+    const char* from;
+    const int valid = q < NA ? piece_a(q < NA ? q : 0, c0, from) : piece_b(q < NA ? 0 : q - NA, c0, from);
+    load_to_lds(valid > 0 ? from : zeros, at);
   };
   constexpr int RA = FAST ? 1 : NA, RB = FAST ? 1 : NB;
   i32x4 va[RA], vb[RB];
-  auto fetch_regs = [&](int64_t c0) {
+  auto fetch_regs = [&](uint32_t c0) {
     if constexpr (!FAST) {
 #pragma unroll
       for (int q = 0; q < NA; ++q) {
         const char* from;
-        const int64_t valid = piece_a(q, c0, from);
-        va[q] = load_piece<T>(from, (int)(valid > EPC ? EPC : valid));
+        const int valid = piece_a(q, c0, from);
+        va[q] = load_piece<T>(from, valid);
       }
 #pragma unroll
       for (int q = 0; q < NB; ++q) {
         const char* from;
-        const int64_t valid = piece_b(q, c0, from);
-        vb[q] = load_piece<T>(from, (int)(valid > EPC ? EPC : valid));
+        const int valid = piece_b(q, c0, from);
+        vb[q] = load_piece<T>(from, valid);
       }
     }
   };
@@ -247,20 +243,23 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     }
   };
 
-  // fragments
-  const int l16 = lane & 15, quarter = lane >> 4;
-  auto turned = [&](const char* tile, int cols, int col16, int slab) -> i32x4 {  // columns 16 col16 .. + 15, 64 bytes of c
+  // operands of 32 lines (columns) and the sub-th 32 bytes of c
+  const int l32 = lane & 31, upper = lane >> 5;
+  auto turned = [&](const char* tile, int cols, int col32, int sub, bool is_j) -> i32x4 {
     if constexpr (SZ == 4) {
       f32x4 v;
+      const int col = col32 * 32 + (is_j ? j_of_row(l32) : l32);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int c = slab * 16 + 4 * quarter + e;
-        v[e] = *reinterpret_cast<const float*>(tile + c * (cols * 4) + ((col16 ^ quarter) * 64) + l16 * 4);
+        const int c = sub * 8 + 4 * upper + e;
+        v[e] = *reinterpret_cast<const float*>(tile + c * (cols * 4) + swizzle_turned<4>(c, col >> 2) * 16 + (col & 3) * 4);
       }
       return __builtin_bit_cast(i32x4, v);
     } else {
-      const int r = l16 >> 2;
-      const char* at = tile + (slab * 32 + 8 * quarter + r) * (cols * 2) + ((col16 ^ (r | ((quarter & 1) << 2))) * 32) + (lane & 3) * 8;
+      // of 16 lanes, lane 4 r + t reads 4 columns of line r, and lane 4 t + e gets the e-th of those t read, of the 4 lines
+      const int c = sub * 16 + 8 * upper + ((lane & 15) >> 2), t = lane & 3, half = (lane >> 4) & 1;
+      const int col = is_j ? j_of_row(16 * half + 4 * t) : 16 * half + 4 * t;
+      const char* at = tile + c * (cols * 2) + swizzle_turned<2>(c, col32 * 4 + (col >> 3)) * 16 + (col & 4) * 2;
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * (cols * 2)));
@@ -270,101 +269,139 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       return v;
     }
   };
-  auto frag_i = [&](const char* st, int f, int slab) -> i32x4 {
-    if constexpr (TA) return turned(st, BI, (wi * FI + f), slab);
-    const int row = (wi * FI + f) * 16 + l16;
-    return *reinterpret_cast<const i32x4*>(st + row * 128 + (((slab * 4 + quarter) ^ swizzle_i(l16)) * 16));
+  auto frag_i = [&](const char* st, int f, int sub) -> i32x4 {
+    if constexpr (TA) return turned(st, BI, wi * FI + f, sub, false);
+    return *reinterpret_cast<const i32x4*>(st + ((wi * FI + f) * 32 + l32) * 128 + (((sub * 2 + upper) ^ swizzle_i(l32)) * 16));
   };
-  // The rows of j go to the matrix instructions in an order that leaves a lane 8 neighbouring columns of the output in two
-  // accumulators: row m of product f is j = 8 (m / 4) + 4 (f % 2) + m % 4 of its 32.
-  auto frag_j = [&](const char* st, int f, int slab) -> i32x4 {
-    if constexpr (TB) return turned(st + BI * 128, BJ, (wj * FJ + f), slab);
-    const int in32 = 8 * (l16 >> 2) + 4 * (f & 1) + (l16 & 3);
-    const int row = (wj * FJ + (f & ~1)) * 16 + in32;
-    return *reinterpret_cast<const i32x4*>(st + BI * 128 + row * 128 + (((slab * 4 + quarter) ^ swizzle_j(in32)) * 16));
+  auto frag_j = [&](const char* st, int f, int sub) -> i32x4 {
+    if constexpr (TB) return turned(st + BI * 128, BJ, wj * FJ + f, sub, true);
+    const int in32 = j_of_row(l32);
+    return *reinterpret_cast<const i32x4*>(st + BI * 128 + ((wj * FJ + f) * 32 + in32) * 128 + (((sub * 2 + upper) ^ swizzle_j(in32)) * 16));
   };
 
   Acc acc[FI][FJ];
 #pragma unroll
   for (int x = 0; x < FI; ++x)
 #pragma unroll
-    for (int y = 0; y < FJ; ++y) acc[x][y] = Acc{0, 0, 0, 0};
+    for (int y = 0; y < FJ; ++y) acc[x][y] = Acc{0};
 
+  // A step is multiplied in four parts of 32 bytes of every line; the operands of the next part are read while one is multiplied.
+  // The one barrier of a step stands in front of its last part, where everybody has read the whole step and the next one, requested
+  // a step ago, has arrived; behind it the step after that is requested into the half that is free, one half of its pieces during
+  // that part and the other during the next.  Reads and requests are dealt out among the products.  Behind the last step all this goes on for nothing (old lines of LDS, pieces of zeros), which is cheaper than
+  // a branch around each.
+  i32x4 ai[2][FI], bj[2][FJ];
+  auto read_one = [&](const char* st, int r, int sub, int set) {
+    if (r < FJ) bj[set][r < FJ ? r : 0] = frag_j(st, r < FJ ? r : 0, sub);
+    else ai[set][r < FJ ? 0 : r - FJ] = frag_i(st, r < FJ ? 0 : r - FJ, sub);
+  };
+  auto multiply = [&](auto sub_c, int next_buf, auto request_c, uint32_t c2, int buf2) {
+    constexpr int sub = decltype(sub_c)::value, set = sub & 1;
+    const char* st = smem + next_buf * STAGE;
+    constexpr int READS = FI + FJ, ROWS = FI >= 2 ? FI / 2 : 1;  // rows of products that reads are dealt out among: the first half
+#pragma unroll
+    for (int x = 0; x < FI; ++x) {
+#pragma unroll
+      for (int part = 0; part < Mma<T>::PARTS; ++part)
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) acc[x][y] = Mma<T>::mul(bj[set][y], ai[set][x], acc[x][y], part);
+#pragma unroll
+      for (int r = 0; r < READS; ++r)
+        if (r * ROWS / READS == x) read_one(st, r, (sub + 1) & 3, set ^ 1);
+      constexpr int HALF = decltype(request_c)::value;  // which half of the pieces is requested, or none
+      if constexpr (HALF >= 0) {
+#pragma unroll
+        for (int q = 0; q < NA + NB; ++q)
+          if (q * (2 * FI) / (NA + NB) == HALF * FI + x) fetch_piece(q, c2, buf2);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  constexpr std::integral_constant<int, 0> sub0{};
+  constexpr std::integral_constant<int, 1> sub1{};
+  constexpr std::integral_constant<int, 2> sub2{};
+  constexpr std::integral_constant<int, 3> sub3{};
+  constexpr std::integral_constant<int, FAST ? 0 : -1> first{};
+  constexpr std::integral_constant<int, FAST ? 1 : -1> second{};
+  constexpr std::integral_constant<int, -1> nothing{};
+  auto fetch_all = [&](uint32_t c0, int buf) {
+    if constexpr (FAST) {
+#pragma unroll
+      for (int q = 0; q < NA + NB; ++q) fetch_piece(q, c0, buf);
+    } else {
+      fetch_regs(c0);
+    }
+  };
   if (nc > 0) {
     find_pairs(0);
-    if constexpr (FAST) {
-      fetch(0, 0);
-    } else {
-      fetch_regs(0);
-      stash(0);
-    }
+    fetch_all(0, 0);
     find_pairs(STEP);
-    int buf = 0;
-    for (int64_t c0 = 0; c0 < nc; c0 += STEP, buf ^= 1) {
-      wait_and_barrier();  // this step has arrived for all, and nobody reads the other half any more
-      const bool more = c0 + STEP < nc;
-      if (more) {
-        if constexpr (FAST) fetch(c0 + STEP, buf ^ 1);
-        else fetch_regs(c0 + STEP);
-        find_pairs(c0 + 2 * STEP);
-      }
-      const char* st = smem + buf * STAGE;
+    stash(0);
+    wait_and_barrier();
 #pragma unroll
-      for (int slab = 0; slab < 2; ++slab) {
-        i32x4 fi[FI], fj[FJ];
+    for (int r = 0; r < FI + FJ; ++r) read_one(smem, r, 0, 0);
+    if constexpr (FAST) {
 #pragma unroll
-        for (int y = 0; y < FJ; ++y) fj[y] = frag_j(st, y, slab);
-#pragma unroll
-        for (int x = 0; x < FI; ++x) fi[x] = frag_i(st, x, slab);
-#pragma unroll
-        for (int x = 0; x < FI; ++x)
-#pragma unroll
-          for (int y = 0; y < FJ; ++y) acc[x][y] = Mma<T>::mul(fj[y], fi[x], acc[x][y]);
-      }
-      if (!FAST && more) stash(buf ^ 1);
+      for (int q = 0; q < NA + NB; ++q) 
+        if (q * (2 * FI) / (NA + NB) < FI) fetch_piece(q, STEP, 1);
+    } else {
+      fetch_regs(STEP);
     }
+    int buf = 0;
+    for (uint32_t c0 = 0; c0 < nc; c0 += STEP, buf ^= 1) {
+      multiply(sub0, buf, second, c0 + STEP, buf ^ 1);
+      multiply(sub1, buf, nothing, 0, 0);
+      find_pairs(c0 + 2 * STEP);
+      multiply(sub2, buf, nothing, 0, 0);
+      stash(buf ^ 1);
+      wait_and_barrier();
+      if constexpr (!FAST) fetch_regs(c0 + 2 * STEP);
+      multiply(sub3, buf ^ 1, first, c0 + 2 * STEP, buf);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);  // nothing may be on its way to LDS when the workgroup ends
   }
 
-  // accumulator register r of a lane: row i = lane % 16, j = 4 (lane / 16) + r of the product (or the order of frag_j)
   const bool whole = (p.ldo | (OP == GRAD_W ? p.stride : 0)) % 8 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
 #pragma unroll
   for (int x = 0; x < FI; ++x) {
-    const int i = (wi * FI + x) * 16 + l16;
+    const int i = (wi * FI + x) * 32 + l32;
     int64_t row;
     if constexpr (OP == GRAD_W) row = i0 + i < iend ? i0 + i : -1;
     else row = row_pair[i];
     if (row < 0) continue;
-    if (OP == GRAD_X && p.named && j0 == 0 && wj == 0 && quarter == 0) p.named[row] = 1;
+    if (OP == GRAD_X && p.named && j0 == 0 && wj == 0 && upper == 0) p.named[row] = 1;
     float sa = 1.f;
-    if constexpr (SZ == 1) sa = p.scale_a[row / p.nprobe];
+    if constexpr (SZ == 1) sa = p.scale_a[p.probe.of((int)row)];
     const int64_t base = (OP == GRAD_W ? (int64_t)g * p.stride : 0) + row * p.ldo;
-    constexpr int RUN = TB ? 4 : 8, PARTS = RUN / 4;  // neighbouring columns of a lane
 #pragma unroll
-    for (int y = 0; y < FJ; y += PARTS) {
-      const int64_t j = j0 + (wj * FJ + y) * 16 + RUN * quarter;
-      float v[RUN];
+    for (int y = 0; y < FJ; ++y) {
 #pragma unroll
-      for (int e = 0; e < RUN; ++e) {
-        v[e] = (float)acc[x][y + e / 4][e % 4];
-        if constexpr (SZ == 1) v[e] = v[e] * sa * p.scale_b[(int64_t)g * p.n + (j + e < width ? j + e : 0)];
-      }
-      if (whole && j + RUN <= width) {
-        if (p.out_dtype == RABITQ_F32) {
+      for (int h = 0; h < 16; h += 8) {  // 8 neighbouring columns
+        const int64_t j = j0 + (wj * FJ + y) * 32 + 16 * upper + h;
+        float v[8];
 #pragma unroll
-          for (int e = 0; e < RUN; e += 4)
-            *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + base + j + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-        } else {
-          typedef uint16_t h16 __attribute__((ext_vector_type(RUN)));
-          h16 h;
-#pragma unroll
-          for (int e = 0; e < RUN; ++e)
-            h[e] = p.out_dtype == RABITQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[e]) : __builtin_bit_cast(uint16_t, (__bf16)v[e]);
-          *reinterpret_cast<h16*>(static_cast<uint16_t*>(p.out) + base + j) = h;
+        for (int e = 0; e < 8; ++e) {
+          v[e] = (float)acc[x][y][h + e];
+          if constexpr (SZ == 1) v[e] = v[e] * sa * p.scale_b[(int64_t)g * p.n + (j + e < width ? j + e : 0)];
         }
-      } else {
+        if (whole && j + 8 <= width) {
+          if (p.out_dtype == RABITQ_F32) {
 #pragma unroll
-        for (int e = 0; e < RUN; ++e)
-          if (j + e < width) store_as(p.out, p.out_dtype, base + j + e, v[e]);
+            for (int e = 0; e < 8; e += 4)
+              *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + base + j + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+          } else {
+            typedef uint16_t h16 __attribute__((ext_vector_type(8)));
+            h16 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              o[e] = p.out_dtype == RABITQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[e]) : __builtin_bit_cast(uint16_t, (__bf16)v[e]);
+            *reinterpret_cast<h16*>(static_cast<uint16_t*>(p.out) + base + j) = o;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (j + e < width) store_as(p.out, p.out_dtype, base + j + e, v[e]);
+        }
       }
     }
   }

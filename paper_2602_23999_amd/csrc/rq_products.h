@@ -5,8 +5,21 @@
 namespace rq {
 
 constexpr int DTYPE_I8 = 3;  // operands only; behind the rabitq_dtype values
-constexpr int64_t MAX_TILES = 1 << 23;  // workgroups of a launch: times 512 threads, what a grid may hold
+constexpr int64_t MAX_GRID = 0xffffffff;  // threads of a launch
 inline int64_t dtype_bytes(int dtype) { return dtype == RABITQ_F32 ? 4 : dtype == DTYPE_I8 ? 1 : 2; }
+
+// x / d for 0 <= x < 2^31, by a multiplication: with 2^(s - 1) < d <= 2^s and m = floor(2^(31 + s) / d) + 1, x m / 2^(31 + s) exceeds
+// x / d by less than x / 2^(31 + s) <= 2^-s <= 1 / d, which no next whole number is nearer than.
+struct Divisor {
+  uint32_t m;
+  int shift;
+  __device__ __forceinline__ int of(int x) const { return (int)(((uint64_t)(uint32_t)x * m) >> shift); }
+};
+inline Divisor divisor(int d) {
+  int s = 0;
+  while (((int64_t)1 << s) < d) ++s;
+  return Divisor{(uint32_t)(((uint64_t)1 << (31 + s)) / (uint64_t)d + 1), 31 + s};
+}
 
 // One product, whichever direction.  `a` has a row per pair or per row of x, `b` is the matrices (forward and dx) or x (dw).
 struct ProductArgs {
@@ -21,9 +34,11 @@ struct ProductArgs {
   const int32_t* pair_ids;    // null: position i is pair i
   int64_t pairs;
   int64_t n;
-  int k, groups, nprobe;
+  int k, groups;
+  Divisor probe;              // by the pairs per row of x
   int out_dtype;
   int64_t tiles;              // of the launch
+  int64_t chunk;              // neighbouring tiles that go to one XCD
   uint8_t* named;             // dx of several probes: set to 1 for every pair a list names, or null
 };
 
