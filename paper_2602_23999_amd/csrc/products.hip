@@ -1,5 +1,5 @@
 // Products by list (forward, gradient of the inputs, gradient of the matrices) and products of int8 codes with scales.
-#include "rq_product_tile.h"
+#include "rq_product_few.h"
 
 namespace rq {
 
@@ -7,20 +7,62 @@ __global__ __launch_bounds__(256) void clear_bytes_kernel(uint8_t* at, int64_t n
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) at[i] = 0;
 }
 
-// dx of several probes: the named pairs' rows in ascending order of the pair.
+// dw in parts: the sums of a list's parts in ascending order; zeros for a list without any.
 template <class T>
+__global__ __launch_bounds__(256) void sum_parts_kernel(ProductArgs p, const float* __restrict__ parts, int part, T* __restrict__ out) {
+  const int64_t elems = p.n * p.k;
+  for (int g = blockIdx.y; g < p.groups; g += gridDim.y) {
+    const Span s = span_of(p, g);
+    const int64_t first = s.begin / part + g, count = s.end > s.begin ? (s.end - s.begin + part - 1) / part : 0;
+    for (int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e0 < elems; e0 += (int64_t)gridDim.x * 1024) {
+      const int here = (int)(elems - e0 < 4 ? elems - e0 : 4);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int64_t c = 0; c < count; ++c) {
+        const float* from = parts + (first + c) * elems + e0;
+        if (here == 4) {
+          float v[4];
+          __builtin_memcpy(v, from, 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += v[e];
+        } else {
+          for (int e = 0; e < here; ++e) sum[e] += from[e];
+        }
+      }
+      int64_t row = e0 / p.k, col = e0 % p.k;
+      for (int e = 0; e < here; ++e) {
+        out[(int64_t)g * p.stride + row * p.ldo + col] = (T)sum[e];
+        if (++col == p.k) { col = 0; ++row; }
+      }
+    }
+  }
+}
+
+// dx of several probes: the named pairs' rows in ascending order of the pair.  A thread takes VEC neighbouring columns (4 where k
+// and the output allow it) of a query.
+template <class T, int VEC>
 __global__ __launch_bounds__(256) void sum_named_kernel(const float* __restrict__ parts, const uint8_t* __restrict__ named, int64_t rows,
                                                         int nprobe, int k, T* __restrict__ out, int64_t ldo) {
-  for (int64_t q = blockIdx.x; q < rows; q += gridDim.x) {
-    for (int j = threadIdx.x; j < k; j += 256) {
-      float sum = 0.f;
-      bool any = false;
-      for (int r = 0; r < nprobe; ++r) {
-        const int64_t pr = q * nprobe + r;
-        if (named[pr]) { sum += parts[pr * k + j]; any = true; }
-      }
-      if (any) out[q * ldo + j] = (T)sum;
+  const int per_row = k / VEC;
+  const int64_t all = rows * per_row;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
+    const int64_t q = id / per_row;
+    const int j = (int)(id - q * per_row) * VEC;
+    float sum[VEC] = {};
+    bool any = false;
+    for (int r = 0; r < nprobe; ++r) {
+      const int64_t pr = q * nprobe + r;
+      if (!named[pr]) continue;
+      any = true;
+      float v[VEC];
+      __builtin_memcpy(v, parts + pr * k + j, 4 * VEC);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e] += v[e];
     }
+    if (!any) continue;
+    T o[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) o[e] = (T)sum[e];
+    __builtin_memcpy(out + q * ldo + j, o, sizeof(T) * VEC);
   }
 }
 
@@ -52,7 +94,7 @@ template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
 static int launch_tiles(ProductArgs p, hipStream_t st) {
   const int64_t width = OP == FORWARD ? p.n : p.k;
   p.chunk = std::max<int64_t>(1, up(width, BJ) / 8);
-  p.tiles = up(width, BJ) * (OP == GRAD_W ? up(p.n, BI) * p.groups : p.pair_off ? p.pairs / BI + p.groups : up(p.pairs, BI));
+  p.tiles = up(width, BJ) * (OP == GRAD_W ? up(p.n, BI) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups) : p.pair_off ? p.pairs / BI + p.groups : up(p.pairs, BI));
   const int64_t grid = up(p.tiles, 8 * p.chunk) * 8 * p.chunk;
   if (grid > MAX_GRID / (64 * WI * WJ)) {
     set_error("too many tiles of work");
@@ -76,8 +118,34 @@ static bool fast_rows(const ProductArgs& p, int op, int dtype) {
          reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && reinterpret_cast<uintptr_t>(p.b) % 16 == 0;
 }
 
+// Whether the forward product goes to the kernel that streams the matrices.  It reads them once per 16 rows, the tile kernel once per 128 or
+// 256; with at most 8 rows per list on average (16 of a single list, whose rows are known) that is once in both, and it needs no
+// LDS and no barriers (64 lists of 2048 x 2048 bf16, 4 rows each: 120 us and 152, 16 rows each: 187 and 182; one query against
+// 200 000 rows of 768 codes: 32 and 68).  Beyond, while the tile kernel would have less than 128 tiles of 128 columns to spread
+// over the chip, it still is the faster up to 48 rows (48 rows, 8192 x 8192 codes: 47 and 69; 32 rows, 50 000 x 768: 21 and 16).
+static bool few_rows(const ProductArgs& p) {
+  const int64_t lists = p.groups;
+  if (p.pairs <= (p.pair_off ? 8 : 16) * lists) return true;
+  return p.pairs <= 48 * lists && std::min(lists, p.pairs) * up(p.n, 128) < 128;
+}
+
+template <class T>
+static int launch_few(const ProductArgs& p, hipStream_t st) {
+  const int64_t grid = (p.pair_off ? p.pairs / 16 + p.groups : up(p.pairs, 16)) * up(p.n, 16);
+  if (grid > MAX_GRID / 256) {
+    set_error("too many tiles of work");
+    return RABITQ_EINVAL;
+  }
+  product_few_kernel<T><<<(unsigned)grid, 256, 0, st>>>(p);
+  RQ_HIP(hipGetLastError());
+  return RABITQ_OK;
+}
+
 template <class T, int OP>
 static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
+  if constexpr (OP == FORWARD) {
+    if (few_rows(p)) return launch_few<T>(p, st);
+  }
   if (!fast_rows(p, OP, dtype)) return launch_tiles<T, OP, 128, 128, 2, 2, false>(p, st);
   const int64_t width = OP == FORWARD ? p.n : p.k;
   const int64_t big = up(width, 256) * (OP == GRAD_W ? up(p.n, 256) * p.groups : p.pairs / 256 + p.groups);
@@ -98,7 +166,29 @@ static int launch_op(const ProductArgs& p, int dtype, hipStream_t st) {
 
 int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<FORWARD>(p, dtype, st); }
 int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<GRAD_X>(p, dtype, st); }
-int launch_product_dw(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<GRAD_W>(p, dtype, st); }
+int dw_part(int64_t pairs, int groups, int64_t n, int64_t k) {
+  const int64_t tiles = up(n, 128) * up(k, 128);
+  if (tiles * groups >= 1024 || pairs < 512) return 0;
+  // as many parts as fill the chip twice, none shorter than 256 positions
+  const int64_t want = std::max<int64_t>(1, up(512, tiles));
+  return (int)(std::max<int64_t>(1, pairs / want / 256) * 256);
+}
+
+int launch_product_dw(const ProductArgs& p, int dtype, float* scratch, hipStream_t st) {
+  ProductArgs q = p;
+  q.part = p.pairs > 0 ? dw_part(p.pairs, p.groups, p.n, p.k) : 0;
+  if (q.part == 0) return launch_op<GRAD_W>(q, dtype, st);
+  q.out = scratch; q.ldo = p.k; q.stride = 0; q.out_dtype = RABITQ_F32;
+  const int rc = launch_op<GRAD_W>(q, dtype, st);
+  if (rc) return rc;
+  const int64_t elems = p.n * p.k;
+  const dim3 grid((unsigned)std::min<int64_t>(up(elems, 1024), 65535), (unsigned)std::min(p.groups, 65535));
+  if (p.out_dtype == RABITQ_F32) sum_parts_kernel<<<grid, 256, 0, st>>>(p, scratch, q.part, (float*)p.out);
+  else if (p.out_dtype == RABITQ_F16) sum_parts_kernel<<<grid, 256, 0, st>>>(p, scratch, q.part, (_Float16*)p.out);
+  else sum_parts_kernel<<<grid, 256, 0, st>>>(p, scratch, q.part, (__bf16*)p.out);
+  RQ_HIP(hipGetLastError());
+  return RABITQ_OK;
+}
 
 int launch_clear_bytes(void* at, int64_t n, hipStream_t st) {
   clear_bytes_kernel<<<(unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, st>>>(static_cast<uint8_t*>(at), n);
@@ -106,14 +196,21 @@ int launch_clear_bytes(void* at, int64_t n, hipStream_t st) {
   return RABITQ_OK;
 }
 
-int launch_sum_named(const float* parts, const uint8_t* named, int64_t rows, int nprobe, int k, void* out, int dtype, int64_t ldo,
-                     hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>(rows, 65536);
-  if (dtype == RABITQ_F32) sum_named_kernel<<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, (float*)out, ldo);
-  else if (dtype == RABITQ_F16) sum_named_kernel<<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, (_Float16*)out, ldo);
-  else sum_named_kernel<<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, (__bf16*)out, ldo);
+template <class T>
+static int sum_named(const float* parts, const uint8_t* named, int64_t rows, int nprobe, int k, T* out, int64_t ldo, hipStream_t st) {
+  const bool four = k % 4 == 0 && ldo % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
+  const unsigned grid = (unsigned)std::min<int64_t>(up(rows * (k / (four ? 4 : 1)), 256), 1 << 20);
+  if (four) sum_named_kernel<T, 4><<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, out, ldo);
+  else sum_named_kernel<T, 1><<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, out, ldo);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
+}
+
+int launch_sum_named(const float* parts, const uint8_t* named, int64_t rows, int nprobe, int k, void* out, int dtype, int64_t ldo,
+                     hipStream_t st) {
+  if (dtype == RABITQ_F32) return sum_named(parts, named, rows, nprobe, k, (float*)out, ldo, st);
+  if (dtype == RABITQ_F16) return sum_named(parts, named, rows, nprobe, k, (_Float16*)out, ldo, st);
+  return sum_named(parts, named, rows, nprobe, k, (__bf16*)out, ldo, st);
 }
 
 int launch_quantize_rows(const void* x, int dtype, int64_t ldx, int64_t rows, int k, int8_t* codes, int64_t ldc, float* scale,

@@ -114,24 +114,26 @@ int rabitq_grouped_matmul_dx(const rabitq_lists* l, int32_t dtype, const void* d
 
 int64_t rabitq_grouped_dw_scratch_bytes(const rabitq_lists* l) {
   const int rc = guarded([&]() -> int { return check_lists("grouped_dw_scratch_bytes", l); });
-  return rc ? rc : 0;
+  if (rc) return rc;
+  const int part = dw_part(l->pairs, l->groups, l->n, l->k);
+  return part == 0 ? 0 : dw_parts(l->pairs, l->groups, part) * l->n * l->k * 4;
 }
 
 int rabitq_grouped_matmul_dw(const rabitq_lists* l, int32_t dtype, const void* dout, int64_t ldd, const void* x, int64_t ldx,
                              void* dw, int64_t ldw, int64_t stride_w, void* scratch, void* stream) {
-  (void)scratch;
   return guarded([&]() -> int {
     const char* call = "grouped_matmul_dw";
     const int rc = check_lists(call, l);
     if (rc) return rc;
     if (!dtype_ok(dtype)) return bad(call, "unknown type");
     if (!ld_ok(ldd, l->n) || !ld_ok(ldx, l->k) || !ld_ok(ldw, l->k) || !stride_ok(l, ldw, stride_w)) return bad(call, "stride out of range");
-    if (!dw || (l->pairs > 0 && (!dout || !x))) return bad(call, "null pointer");
+    const bool in_parts = dw_part(l->pairs, l->groups, l->n, l->k) != 0;
+    if (!dw || (l->pairs > 0 && (!dout || !x)) || (in_parts && !scratch)) return bad(call, "null pointer");
     const int64_t sz = dtype_bytes(dtype);
-    if (!aligned(dout, sz) || !aligned(x, sz) || !aligned(dw, sz)) return bad(call, "pointer not aligned to its type");
+    if (!aligned(dout, sz) || !aligned(x, sz) || !aligned(dw, sz) || !aligned(scratch, 16)) return bad(call, "pointer not aligned to its type");
     ProductArgs p = args_of(l);
     p.a = dout; p.lda = ldd; p.b = x; p.ldb = ldx; p.out = dw; p.ldo = ldw; p.stride = stride_w; p.out_dtype = dtype;
-    return launch_product_dw(p, dtype, (hipStream_t)stream);
+    return launch_product_dw(p, dtype, static_cast<float*>(scratch), (hipStream_t)stream);
   });
 }
 

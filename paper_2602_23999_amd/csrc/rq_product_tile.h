@@ -132,12 +132,25 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   Span s;
   int64_t i0, iend;
   uint32_t nc;  // length of the contraction, below 2^31: positions and pairs are 32-bit numbers
+  void* out = p.out;
   if constexpr (OP == GRAD_W) {
     const int64_t it = (p.n + BI - 1) / BI;
-    g = (int)(tile / it);
-    s = span_of(p, g);
+    const int64_t unit = tile / it;  // a list, or (p.part > 0) a part of p.part positions of one
     i0 = tile % it * BI;
     iend = p.n;
+    if (p.part > 0) {
+      g = list_of_tile(p, unit, p.part, lane);
+      s = span_of(p, g);
+      const int64_t begin = s.begin + (unit - (s.begin / p.part + g)) * p.part;
+      if (begin < s.begin || begin >= s.end) return;
+      s.end = min(s.end, begin + p.part);
+      s.begin = begin;
+      g = 0;
+      out = static_cast<float*>(p.out) + unit * p.n * p.k;
+    } else {
+      g = (int)unit;
+      s = span_of(p, g);
+    }
     nc = s.end > s.begin ? (uint32_t)(s.end - s.begin) : 0;
   } else {
     g = p.pair_off ? list_of_tile(p, tile, BI, lane) : 0;
@@ -361,49 +374,62 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     __builtin_amdgcn_s_waitcnt(0x0070);  // nothing may be on its way to LDS when the workgroup ends
   }
 
-  const bool whole = (p.ldo | (OP == GRAD_W ? p.stride : 0)) % 8 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
+  // A lane has 16 neighbouring columns of a row, so a store of its own would touch 32 rows for 16 bytes each.  The wavefront's 32
+  // rows go through LDS instead (its own part of it, as fp32, pieces of 16 bytes swizzled by the row) and out in whole rows of COLS.
+  constexpr int COLS = FJ * 32, PIECES = COLS / 4;  // of a row: a power of two
+  static_assert(32 * COLS * 4 * WI * WJ <= 2 * STAGE && (PIECES & (PIECES - 1)) == 0 && PIECES >= 8);
+  const int64_t ldo = p.ldo;
+  const int each = p.out_dtype == RABITQ_F32 ? 4 : 8;  // columns that a lane stores at once
+  const bool whole = (ldo | (OP == GRAD_W ? p.stride : 0)) % each == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
+  f32x4* mine = reinterpret_cast<f32x4*>(smem) + wave * (32 * PIECES);
+  __syncthreads();  // (the last operands have been read)
 #pragma unroll
   for (int x = 0; x < FI; ++x) {
-    const int i = (wi * FI + x) * 32 + l32;
-    int64_t row;
-    if constexpr (OP == GRAD_W) row = i0 + i < iend ? i0 + i : -1;
-    else row = row_pair[i];
-    if (row < 0) continue;
-    if (OP == GRAD_X && p.named && j0 == 0 && wj == 0 && upper == 0) p.named[row] = 1;
-    float sa = 1.f;
-    if constexpr (SZ == 1) sa = p.scale_a[p.probe.of((int)row)];
-    const int64_t base = (OP == GRAD_W ? (int64_t)g * p.stride : 0) + row * p.ldo;
 #pragma unroll
-    for (int y = 0; y < FJ; ++y) {
+    for (int y = 0; y < FJ; ++y)
 #pragma unroll
-      for (int h = 0; h < 16; h += 8) {  // 8 neighbouring columns
-        const int64_t j = j0 + (wj * FJ + y) * 32 + 16 * upper + h;
-        float v[8];
+      for (int h = 0; h < 4; ++h)
+        mine[l32 * PIECES + ((y * 8 + upper * 4 + h) ^ (l32 & (PIECES - 1)))] =
+            f32x4{(float)acc[x][y][4 * h], (float)acc[x][y][4 * h + 1], (float)acc[x][y][4 * h + 2], (float)acc[x][y][4 * h + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int per_row = COLS / each, rows_at_once = 64 / per_row;
+    const int col = lane % per_row * each;
+    const int64_t j = j0 + wj * COLS + col;
+    for (int r = lane / per_row; r < 32; r += rows_at_once) {
+      const int i = (wi * FI + x) * 32 + r;
+      int64_t row;
+      if constexpr (OP == GRAD_W) row = i0 + i < iend ? i0 + i : -1;
+      else row = row_pair[i];
+      if (row < 0) continue;
+      if (OP == GRAD_X && p.named && j == 0) p.named[row] = 1;
+      if (j >= width) continue;
+      float sa = 1.f;
+      if constexpr (SZ == 1) sa = p.scale_a[p.probe.of((int)row)];
+      const int64_t at = (OP == GRAD_W ? (int64_t)g * p.stride : 0) + row * ldo + j;
+      f32x4 lo = mine[r * PIECES + ((col >> 2) ^ (r & (PIECES - 1)))];
+      f32x4 hi = lo;
+      if (each == 8) hi = mine[r * PIECES + (((col >> 2) + 1) ^ (r & (PIECES - 1)))];
+      if constexpr (SZ == 1) {
+        const float* sb = p.scale_b + (int64_t)g * p.n + j;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] = (float)acc[x][y][h + e];
-          if constexpr (SZ == 1) v[e] = v[e] * sa * p.scale_b[(int64_t)g * p.n + (j + e < width ? j + e : 0)];
-        }
-        if (whole && j + 8 <= width) {
-          if (p.out_dtype == RABITQ_F32) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 4)
-              *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + base + j + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-          } else {
-            typedef uint16_t h16 __attribute__((ext_vector_type(8)));
-            h16 o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              o[e] = p.out_dtype == RABITQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[e]) : __builtin_bit_cast(uint16_t, (__bf16)v[e]);
-            *reinterpret_cast<h16*>(static_cast<uint16_t*>(p.out) + base + j) = o;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (j + e < width) store_as(p.out, p.out_dtype, base + j + e, v[e]);
+        for (int e = 0; e < 4; ++e) {
+          lo[e] = lo[e] * sa * (j + e < width ? sb[e] : 0.f);
+          if (each == 8) hi[e] = hi[e] * sa * (j + 4 + e < width ? sb[4 + e] : 0.f);
         }
       }
+      if (whole && j + each <= width) {
+        if (p.out_dtype == RABITQ_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = lo;
+        else if (p.out_dtype == RABITQ_F16) *reinterpret_cast<f16x8*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), f16x8);
+        else *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < each && j + e < width) store_as(out, p.out_dtype, at + e, e < 4 ? lo[e % 4] : hi[e % 4]);
+      }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
