@@ -100,7 +100,7 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
-  const size_t lds = 2 * (BI + BJ) * 128 + BI * sizeof(int);
+  const size_t lds = 2 * (BI + BJ) * 128 + BI * (sizeof(int) + sizeof(float));
   auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, FAST>;
   static const hipError_t granted =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -141,16 +141,33 @@ static int launch_few(const ProductArgs& p, hipStream_t st) {
   return RABITQ_OK;
 }
 
+// The edge of the tile.  A larger one moves fewer bytes per product (8192 x 8192 x 4096 codes: 521, 365, 277 us for 64, 128, 256), but
+// leaves the chip idle when there are few tiles (2048 x 4096 x 4096: 64, 46, 56; 1000 x 4096 x 4096: 33, 34, 53), multiplies rows
+// that are not there where lists are shorter than it (64 lists of 64 rows, 2048 x 2048 bf16: 150, 170, 182; of 128 rows: 200, 190,
+// 202; of 256 rows: 320, 252, 252), and has less to overlap its start and end with where the contraction is one or two steps
+// (10 000 x 1024 x 128 codes: 17, 21, 19).  For dw the rows and columns are those of the matrices and always there.
+static int tile_size(const ProductArgs& p, int op, int size) {
+  const int64_t width = op == FORWARD ? p.n : p.k;
+  const int64_t rows = op == GRAD_W ? p.n : p.pairs / p.groups;  // of a list, on average
+  const int64_t lists = op == GRAD_W && p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups;
+  const int64_t contraction = op == FORWARD ? p.k : op == GRAD_X ? p.n : p.part > 0 ? p.part : p.pairs / p.groups;
+  if (contraction * size < 512) return 64;
+  if (rows >= 256 && up(rows, 256) * up(width, 256) * lists >= 256) return 256;
+  if (rows >= 128 && up(rows, 128) * up(width, 128) * lists >= 512) return 128;
+  return 64;
+}
+
 template <class T, int OP>
 static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
     if (few_rows(p)) return launch_few<T>(p, st);
   }
   if (!fast_rows(p, OP, dtype)) return launch_tiles<T, OP, 128, 128, 2, 2, false>(p, st);
-  const int64_t width = OP == FORWARD ? p.n : p.k;
-  const int64_t big = up(width, 256) * (OP == GRAD_W ? up(p.n, 256) * p.groups : p.pairs / 256 + p.groups);
-  if (big >= 512) return launch_tiles<T, OP, 256, 256, 2, 4, true>(p, st);
-  return launch_tiles<T, OP, 128, 128, 2, 2, true>(p, st);
+  switch (tile_size(p, OP, sizeof(T))) {
+    case 256: return launch_tiles<T, OP, 256, 256, 2, 4, true>(p, st);
+    case 128: return launch_tiles<T, OP, 128, 128, 2, 2, true>(p, st);
+  }
+  return launch_tiles<T, OP, 64, 64, 2, 2, true>(p, st);
 }
 
 template <int OP>

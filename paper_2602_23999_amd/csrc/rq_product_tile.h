@@ -78,9 +78,11 @@ __device__ __forceinline__ void wait_and_barrier() {
 // (2) lines at a time.
 __device__ __forceinline__ int swizzle_i(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int swizzle_j(int row) { return ((row >> 1) & 1) | ((row >> 3) & 2) | (row & 4); }  // of m, row = j_of_row(m)
-template <int SIZE>
-__device__ __forceinline__ int swizzle_turned(int c, int piece) {  // of a line of one c
+template <int SIZE, int PIECES>  // of a line of one c, of so many pieces
+__device__ __forceinline__ int swizzle_turned(int c, int piece) {
+  static_assert(PIECES == 8 || PIECES % 16 == 0);
   if constexpr (SIZE == 4) return piece ^ (((c >> 2) & 1) << 3);
+  else if constexpr (PIECES == 8) return piece ^ ((c & 2) << 1);  // (odd lines start in the other half of the banks)
   else return piece ^ ((c & 3) << 2);
 }
 
@@ -114,6 +116,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   using Acc = typename Mma<T>::Acc;
   extern __shared__ __align__(16) char smem[];
   int* row_pair = reinterpret_cast<int*>(smem + 2 * STAGE);  // [BI] pair of every row, or -1
+  float* row_scale = reinterpret_cast<float*>(row_pair + BI);  // [BI] codes only
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
 
@@ -159,7 +162,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     iend = s.end;
     if (i0 < s.begin || i0 >= iend) return;
     nc = OP == FORWARD ? p.k : (uint32_t)p.n;
-    for (int i = tid; i < BI; i += NT) row_pair[i] = i0 + i < iend ? (int)pair_at(p, i0 + i) : -1;
+    for (int i = tid; i < BI; i += NT) {
+      const int pr = i0 + i < iend ? (int)pair_at(p, i0 + i) : -1;
+      row_pair[i] = pr;
+      if constexpr (SZ == 1) row_scale[i] = pr < 0 ? 0.f : p.scale_a[p.probe.of(pr)];
+    }
     __syncthreads();
   }
   const char* a = static_cast<const char*>(p.a);
@@ -202,7 +209,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       from = pa[q] + (uint64_t)c0 * SZ;
       return c0 + ca < nc ? (int)(nc - c0 - ca) : 0;
     } else {
-      const int col = swizzle_turned<SZ>((tid + q * NT) / PA, (tid + q * NT) % PA) * EPC;
+      const int col = swizzle_turned<SZ, PA>((tid + q * NT) / PA, (tid + q * NT) % PA) * EPC;
       from = a + ((int64_t)pairs_next[q] * p.lda + i0 + col) * SZ;
       return pairs_next[q] < 0 ? 0 : (int)(iend - i0) - col;
     }
@@ -212,11 +219,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       from = pb + ((int64_t)(q * (NT / 8)) * p.ldb + c0) * SZ;
       return line + q * (NT / 8) < jleft && c0 + cb < nc ? (int)(nc - c0 - cb) : 0;
     } else if constexpr (OP == GRAD_X) {
-      const int c = (tid + q * NT) / PB, piece = swizzle_turned<SZ>(c, (tid + q * NT) % PB);
+      const int c = (tid + q * NT) / PB, piece = swizzle_turned<SZ, PB>(c, (tid + q * NT) % PB);
       from = pb + ((int64_t)(c0 + q * (NT / PB)) * p.ldb + piece * EPC) * SZ;
       return c0 + c < nc ? jleft - piece * EPC : 0;
     } else {
-      const int col = swizzle_turned<SZ>((tid + q * NT) / PB, (tid + q * NT) % PB) * EPC;
+      const int col = swizzle_turned<SZ, PB>((tid + q * NT) / PB, (tid + q * NT) % PB) * EPC;
       from = b + ((int64_t)p.probe.of(pairs_next[q]) * p.ldb + j0 + col) * SZ;
       return pairs_next[q] < 0 ? 0 : jleft - col;
     }
@@ -258,21 +265,22 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
 
   // operands of 32 lines (columns) and the sub-th 32 bytes of c
   const int l32 = lane & 31, upper = lane >> 5;
-  auto turned = [&](const char* tile, int cols, int col32, int sub, bool is_j) -> i32x4 {
+  auto turned = [&](const char* tile, auto cols_c, int col32, int sub, bool is_j) -> i32x4 {
+    constexpr int cols = decltype(cols_c)::value;
     if constexpr (SZ == 4) {
       f32x4 v;
       const int col = col32 * 32 + (is_j ? j_of_row(l32) : l32);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int c = sub * 8 + 4 * upper + e;
-        v[e] = *reinterpret_cast<const float*>(tile + c * (cols * 4) + swizzle_turned<4>(c, col >> 2) * 16 + (col & 3) * 4);
+        v[e] = *reinterpret_cast<const float*>(tile + c * (cols * 4) + swizzle_turned<4, cols / 4>(c, col >> 2) * 16 + (col & 3) * 4);
       }
       return __builtin_bit_cast(i32x4, v);
     } else {
       // of 16 lanes, lane 4 r + t reads 4 columns of line r, and lane 4 t + e gets the e-th of those t read, of the 4 lines
       const int c = sub * 16 + 8 * upper + ((lane & 15) >> 2), t = lane & 3, half = (lane >> 4) & 1;
       const int col = is_j ? j_of_row(16 * half + 4 * t) : 16 * half + 4 * t;
-      const char* at = tile + c * (cols * 2) + swizzle_turned<2>(c, col32 * 4 + (col >> 3)) * 16 + (col & 4) * 2;
+      const char* at = tile + c * (cols * 2) + swizzle_turned<2, cols / 8>(c, col32 * 4 + (col >> 3)) * 16 + (col & 4) * 2;
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * (cols * 2)));
@@ -283,11 +291,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     }
   };
   auto frag_i = [&](const char* st, int f, int sub) -> i32x4 {
-    if constexpr (TA) return turned(st, BI, wi * FI + f, sub, false);
+    if constexpr (TA) return turned(st, std::integral_constant<int, BI>{}, wi * FI + f, sub, false);
     return *reinterpret_cast<const i32x4*>(st + ((wi * FI + f) * 32 + l32) * 128 + (((sub * 2 + upper) ^ swizzle_i(l32)) * 16));
   };
   auto frag_j = [&](const char* st, int f, int sub) -> i32x4 {
-    if constexpr (TB) return turned(st + BI * 128, BJ, wj * FJ + f, sub, true);
+    if constexpr (TB) return turned(st + BI * 128, std::integral_constant<int, BJ>{}, wj * FJ + f, sub, true);
     const int in32 = j_of_row(l32);
     return *reinterpret_cast<const i32x4*>(st + BI * 128 + ((wj * FJ + f) * 32 + in32) * 128 + (((sub * 2 + upper) ^ swizzle_j(in32)) * 16));
   };
@@ -325,7 +333,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       if constexpr (HALF >= 0) {
 #pragma unroll
         for (int q = 0; q < NA + NB; ++q)
-          if (q * (2 * FI) / (NA + NB) == HALF * FI + x) fetch_piece(q, c2, buf2);
+          if (q * (2 * FI) / (NA + NB) == HALF * FI + x && (BI >= 256 || c2 < nc)) fetch_piece(q, c2, buf2);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -382,6 +390,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   const int each = p.out_dtype == RABITQ_F32 ? 4 : 8;  // columns that a lane stores at once
   const bool whole = (ldo | (OP == GRAD_W ? p.stride : 0)) % each == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
   f32x4* mine = reinterpret_cast<f32x4*>(smem) + wave * (32 * PIECES);
+  const int per_row = COLS / each, rows_at_once = 64 / per_row;
+  const int col = lane % per_row * each;
+  const int64_t j = j0 + wj * COLS + col;
+  float sb[SZ == 1 ? 8 : 1];  // of this lane's columns
+  if constexpr (SZ == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sb[e] = e < each && j + e < width ? p.scale_b[(int64_t)g * p.n + j + e] : 0.f;
+  }
   __syncthreads();  // (the last operands have been read)
 #pragma unroll
   for (int x = 0; x < FI; ++x) {
@@ -393,9 +409,6 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
             f32x4{(float)acc[x][y][4 * h], (float)acc[x][y][4 * h + 1], (float)acc[x][y][4 * h + 2], (float)acc[x][y][4 * h + 3]};
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int per_row = COLS / each, rows_at_once = 64 / per_row;
-    const int col = lane % per_row * each;
-    const int64_t j = j0 + wj * COLS + col;
     for (int r = lane / per_row; r < 32; r += rows_at_once) {
       const int i = (wi * FI + x) * 32 + r;
       int64_t row;
@@ -404,18 +417,16 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       if (row < 0) continue;
       if (OP == GRAD_X && p.named && j == 0) p.named[row] = 1;
       if (j >= width) continue;
-      float sa = 1.f;
-      if constexpr (SZ == 1) sa = p.scale_a[p.probe.of((int)row)];
       const int64_t at = (OP == GRAD_W ? (int64_t)g * p.stride : 0) + row * ldo + j;
       f32x4 lo = mine[r * PIECES + ((col >> 2) ^ (r & (PIECES - 1)))];
       f32x4 hi = lo;
       if (each == 8) hi = mine[r * PIECES + (((col >> 2) + 1) ^ (r & (PIECES - 1)))];
       if constexpr (SZ == 1) {
-        const float* sb = p.scale_b + (int64_t)g * p.n + j;
+        const float sa = row_scale[i];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          lo[e] = lo[e] * sa * (j + e < width ? sb[e] : 0.f);
-          if (each == 8) hi[e] = hi[e] * sa * (j + 4 + e < width ? sb[4 + e] : 0.f);
+          lo[e] = lo[e] * sa * sb[e];
+          hi[e] = hi[e] * sa * sb[4 + e];
         }
       }
       if (whole && j + each <= width) {

@@ -378,17 +378,22 @@ DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 def _here(t: torch.Tensor, dtype, dims: int, what: str):
-    """A tensor of the current device with `dims` dimensions, whose last one is contiguous and whose rows do not overlap."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
+    """A tensor of the current device with `dims` dimensions, whose last one is contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
         raise RabitqError(f"{what}: expected a tensor on the current CUDA device")
-    if t.dtype != dtype or t.dim() != dims:
+    if t.dtype is not dtype or t.dim() != dims:
         raise RabitqError(f"{what}: expected {dims} dimensions of {dtype}, got {t.dim()} of {t.dtype}")
     if t.requires_grad and torch.is_grad_enabled():
         raise RabitqError(f"{what} requires a gradient, which this call does not record: pass it detached or under "
                           "torch.no_grad()")
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
         raise RabitqError(f"{what}: the last dimension must be contiguous")
     return t
+
+
+def _current_stream(t: torch.Tensor) -> int:
+    """_stream() for a tensor that _here has seen; a third of its time, which counts beside kernels of a few microseconds."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -409,18 +414,19 @@ def _float_type(t: torch.Tensor, what: str):
 def _output(out, shape, dtype, device, what="out"):
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(_here(out, dtype, len(shape), what).shape) != tuple(shape):
+    if _here(out, dtype, len(shape), what).shape != shape:
         raise RabitqError(f"{what}: expected the shape {tuple(shape)}, got {tuple(out.shape)}")
     return out
 
 
 def _lists_of(groups: int, n: int, k: int, pairs: int, nprobe: int, pair_off, pair_ids) -> "_Lists":
-    _here(pair_off, torch.int32, 1, "pair_off")
-    if pair_off.shape[0] != groups + 1:
+    if _here(pair_off, torch.int32, 1, "pair_off").shape[0] != groups + 1:
         raise RabitqError(f"pair_off must hold {groups + 1} offsets, got {pair_off.shape[0]}")
-    if pair_ids is not None and _here(pair_ids, torch.int32, 1, "pair_ids").shape[0] != pairs:
+    if pair_ids is None:
+        return _Lists(groups, nprobe, pairs, n, k, pair_off.data_ptr(), None)
+    if _here(pair_ids, torch.int32, 1, "pair_ids").shape[0] != pairs:
         raise RabitqError(f"pair_ids must hold {pairs} pairs, got {pair_ids.shape[0]}")
-    return _Lists(groups, nprobe, pairs, n, k, pair_off.data_ptr(), None if pair_ids is None else pair_ids.data_ptr())
+    return _Lists(groups, nprobe, pairs, n, k, pair_off.data_ptr(), pair_ids.data_ptr())
 
 
 def _nprobe(nprobe) -> int:
@@ -430,7 +436,7 @@ def _nprobe(nprobe) -> int:
 
 
 def _scales(t, shape, what):
-    if tuple(_here(t, torch.float32, len(shape), what).shape) != tuple(shape) or not t.is_contiguous():
+    if _here(t, torch.float32, len(shape), what).shape != shape or not t.is_contiguous():
         raise RabitqError(f"{what}: expected a contiguous tensor of the shape {tuple(shape)}")
     return t.data_ptr()
 
@@ -453,7 +459,7 @@ def grouped_matmul(x, w, pair_off, pair_ids=None, nprobe: int = 1, out=None):
     ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids)
     out = _output(out, (nq * nprobe, n), dt, x.device)
     _check(load_library().rabitq_grouped_matmul(C.byref(ls), DTYPES[dt], x.data_ptr(), _ld(x), w.data_ptr(), _ld(w),
-                                                _matrix_stride(w), out.data_ptr(), _ld(out), _stream()))
+                                                _matrix_stride(w), out.data_ptr(), _ld(out), _current_stream(out)))
     return out
 
 
@@ -473,7 +479,8 @@ def grouped_matmul_dx(dout, w, pair_off, pair_ids=None, nprobe: int = 1, out=Non
     scratch = _scratch(lib.rabitq_grouped_dx_scratch_bytes(C.byref(ls)), dout.device)
     _check(lib.rabitq_grouped_matmul_dx(C.byref(ls), DTYPES[dt], dout.data_ptr(), _ld(dout), w.data_ptr(), _ld(w),
                                         _matrix_stride(w), out.data_ptr(), _ld(out),
-                                        None if scratch is None else scratch.data_ptr(), _stream()))
+                                        None if scratch is None else scratch.data_ptr(),
+                                        _current_stream(out)))
     return out
 
 
@@ -493,7 +500,8 @@ def grouped_matmul_dw(dout, x, pair_off, pair_ids=None, nprobe: int = 1, out=Non
     scratch = _scratch(lib.rabitq_grouped_dw_scratch_bytes(C.byref(ls)), dout.device)
     _check(lib.rabitq_grouped_matmul_dw(C.byref(ls), DTYPES[dt], dout.data_ptr(), _ld(dout), x.data_ptr(), _ld(x),
                                         out.data_ptr(), _ld(out), _matrix_stride(out),
-                                        None if scratch is None else scratch.data_ptr(), _stream()))
+                                        None if scratch is None else scratch.data_ptr(),
+                                        _current_stream(out)))
     return out
 
 
@@ -506,7 +514,7 @@ def quantize_rows(x, codes=None, scale=None):
     codes = _output(codes, (rows, k), torch.int8, x.device, "codes")
     scale = _output(scale, (rows,), torch.float32, x.device, "scale")
     _check(load_library().rabitq_quantize_rows(x.data_ptr(), DTYPES[dt], _ld(x), rows, k, codes.data_ptr(), _ld(codes),
-                                               _scales(scale, (rows,), "scale"), _stream()))
+                                               _scales(scale, (rows,), "scale"), _current_stream(codes)))
     return codes, scale
 
 
@@ -521,7 +529,7 @@ def matmul_i8(a, scale_a, b, scale_b, out_dtype=torch.float32, out=None):
     out = _output(out, (m, n), out_dtype, a.device)
     _check(load_library().rabitq_matmul_i8(a.data_ptr(), _ld(a), _scales(scale_a, (m,), "scale_a"), b.data_ptr(), _ld(b),
                                            _scales(scale_b, (n,), "scale_b"), m, n, k, out.data_ptr(), DTYPES[out_dtype],
-                                           _ld(out), _stream()))
+                                           _ld(out), _current_stream(out)))
     return out
 
 
@@ -538,7 +546,7 @@ def grouped_matmul_i8(x, scale_x, w, scale_w, pair_off, pair_ids=None, nprobe: i
     out = _output(out, (nq * nprobe, n), out_dtype, x.device)
     _check(load_library().rabitq_grouped_matmul_i8(
         C.byref(ls), x.data_ptr(), _ld(x), _scales(scale_x, (nq,), "scale_x"), w.data_ptr(), _ld(w), _matrix_stride(w),
-        _scales(scale_w, (g, n), "scale_w"), out.data_ptr(), DTYPES[out_dtype], _ld(out), _stream()))
+        _scales(scale_w, (g, n), "scale_w"), out.data_ptr(), DTYPES[out_dtype], _ld(out), _current_stream(out)))
     return out
 
 
