@@ -66,28 +66,6 @@ __global__ __launch_bounds__(256) void sum_named_kernel(const float* __restrict_
   }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int k,
-                                                            int8_t* __restrict__ codes, int64_t ldc, float* __restrict__ scale) {
-  __shared__ uint32_t top_s[4];
-  const int tid = threadIdx.x;
-  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
-    uint32_t top = 0;  // |x| as bits: they order as the values do, infinity and NaN above all numbers
-    for (int j = tid; j < k; j += 256) top = max(top, __float_as_uint(to_f32(x[i * ldx + j])) & 0x7fffffffu);
-    for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    if ((tid & 63) == 0) top_s[tid >> 6] = top;
-    __syncthreads();
-    top = max(max(top_s[0], top_s[1]), max(top_s[2], top_s[3]));
-    __syncthreads();
-    const bool bad = top >= 0x7f800000u;
-    float sc = __uint_as_float(top) / 127.0f;
-    if (sc == 0.f) sc = 1.0f;
-    for (int j = tid; j < k; j += 256)
-      codes[i * ldc + j] = bad ? 0 : (int8_t)(int)rint((double)to_f32(x[i * ldx + j]) / (double)sc);
-    if (tid == 0) scale[i] = bad ? __uint_as_float(0x7fc00000u) : sc;
-  }
-}
-
 static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
 template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
@@ -162,8 +140,10 @@ static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
     if (few_rows(p)) return launch_few<T>(p, st);
   }
-  if (!fast_rows(p, OP, dtype)) return launch_tiles<T, OP, 128, 128, 2, 2, false>(p, st);
-  switch (tile_size(p, OP, sizeof(T))) {
+  const int edge = tile_size(p, OP, sizeof(T));
+  if (!fast_rows(p, OP, dtype))
+    return edge > 64 ? launch_tiles<T, OP, 128, 128, 2, 2, false>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, false>(p, st);
+  switch (edge) {
     case 256: return launch_tiles<T, OP, 256, 256, 2, 4, true>(p, st);
     case 128: return launch_tiles<T, OP, 128, 128, 2, 2, true>(p, st);
   }
@@ -228,16 +208,6 @@ int launch_sum_named(const float* parts, const uint8_t* named, int64_t rows, int
   if (dtype == RABITQ_F32) return sum_named(parts, named, rows, nprobe, k, (float*)out, ldo, st);
   if (dtype == RABITQ_F16) return sum_named(parts, named, rows, nprobe, k, (_Float16*)out, ldo, st);
   return sum_named(parts, named, rows, nprobe, k, (__bf16*)out, ldo, st);
-}
-
-int launch_quantize_rows(const void* x, int dtype, int64_t ldx, int64_t rows, int k, int8_t* codes, int64_t ldc, float* scale,
-                         hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>(rows, 65536);
-  if (dtype == RABITQ_F32) quantize_rows_kernel<<<grid, 256, 0, st>>>((const float*)x, ldx, rows, k, codes, ldc, scale);
-  else if (dtype == RABITQ_F16) quantize_rows_kernel<<<grid, 256, 0, st>>>((const _Float16*)x, ldx, rows, k, codes, ldc, scale);
-  else quantize_rows_kernel<<<grid, 256, 0, st>>>((const __bf16*)x, ldx, rows, k, codes, ldc, scale);
-  RQ_HIP(hipGetLastError());
-  return RABITQ_OK;
 }
 
 }  // namespace rq

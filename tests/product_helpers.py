@@ -98,7 +98,7 @@ def codes64(x):
     scale = (top / 127).float()
     scale = torch.where(scale == 0, torch.ones_like(scale), scale)
     bad = ~torch.isfinite(x64).all(1)
-    codes = torch.where(bad[:, None], torch.zeros_like(x64), torch.round(x64 / scale.double()[:, None]))
+    codes = torch.where(bad[:, None], torch.zeros_like(x64), torch.round(x64 / scale.double()[:, None]).clamp(-127, 127))
     return codes.to(torch.int8), torch.where(bad, torch.full_like(scale, float("nan")), scale)
 
 

@@ -121,7 +121,8 @@ def test_matmul_i8_scales_that_are_no_numbers():
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-@pytest.mark.parametrize("rows,k", [(1, 1), (3, 7), (8, 1024), (5, 1000), (300, 96), (2, 20001), (1000, 256), (64, 4096)])
+@pytest.mark.parametrize("rows,k", [(1, 1), (3, 7), (8, 1024), (5, 1000), (300, 96), (2, 20001), (1000, 256), (64, 4096), (7, 1023),
+                                    (6, 2048), (6, 2049), (5, 8191), (3, 8193)])
 def test_quantize_rows(rows, k, dtype):
     x = numbers(k, (rows, k), torch.float32)
     x[rows // 2] *= 1000.0
@@ -152,6 +153,18 @@ def test_quantize_rows_ties_zeros_and_no_numbers(dtype):
     ok = ~want_scale.isnan()
     assert torch.equal(scale.cpu()[ok], want_scale[ok])
     assert scale[3] == 1 and (codes[3:7] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_quantize_rows_of_denormal_numbers(dtype):
+    # multiples of the smallest number of the type, up to 1000 and up to where the scale is a normal number again
+    step = 2.0 ** -149 if dtype == torch.float32 else 2.0 ** -133
+    g = torch.Generator().manual_seed(4)
+    rows = [torch.randint(-top, top + 1, (200,), generator=g).double() * step for top in (1, 63, 64, 127, 128, 190, 191, 255, 1000)]
+    x = torch.stack(rows + [numbers(5, (200,), torch.float32).double() * 2.0 ** -e for e in (100, 120, 126, 130)]).to(dtype)
+    codes, scale = rabitq.quantize_rows(x.cuda())
+    want, want_scale = codes64(x)
+    assert torch.equal(scale.cpu(), want_scale) and torch.equal(codes.cpu(), want)
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
