@@ -7,18 +7,19 @@ __global__ __launch_bounds__(256) void clear_bytes_kernel(uint8_t* at, int64_t n
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) at[i] = 0;
 }
 
-// dw in parts: the sums of a list's parts in ascending order; zeros for a list without any.
+// dw in parts: the sums of the parts of a list that has several, in ascending order; zeros for a list without positions.
 template <class T>
-__global__ __launch_bounds__(256) void sum_parts_kernel(ProductArgs p, const float* __restrict__ parts, int part, T* __restrict__ out) {
+__global__ __launch_bounds__(256) void sum_parts_kernel(ProductArgs p, T* __restrict__ out) {
   const int64_t elems = p.n * p.k;
   for (int g = blockIdx.y; g < p.groups; g += gridDim.y) {
     const Span s = span_of(p, g);
-    const int64_t first = s.begin / part + g, count = s.end > s.begin ? (s.end - s.begin + part - 1) / part : 0;
+    const int64_t first = s.begin / p.part + g, count = s.end > s.begin ? (s.end - s.begin + p.part - 1) / p.part : 0;
+    if (count == 1) continue;
     for (int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e0 < elems; e0 += (int64_t)gridDim.x * 1024) {
       const int here = (int)(elems - e0 < 4 ? elems - e0 : 4);
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
       for (int64_t c = 0; c < count; ++c) {
-        const float* from = parts + (first + c) * elems + e0;
+        const float* from = p.parts + (first + c) * elems + e0;
         if (here == 4) {
           float v[4];
           __builtin_memcpy(v, from, 16);
@@ -78,7 +79,7 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
-  const size_t lds = 2 * (BI + BJ) * 128 + BI * (sizeof(int) + sizeof(float));
+  const size_t lds = 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int) : BI * (sizeof(int) + sizeof(float)));
   auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, FAST>;
   static const hipError_t granted =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -163,26 +164,27 @@ static int launch_op(const ProductArgs& p, int dtype, hipStream_t st) {
 
 int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<FORWARD>(p, dtype, st); }
 int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<GRAD_X>(p, dtype, st); }
+// Without parts a list occupies one workgroup per tile of its matrix, however long it is, so parts are for launches that would
+// leave places of the chip free: fewer than 512 tiles of 128 x 128 (two for each compute unit).  A part is as long as fills those places,
+// at least 512 positions, so that adding up costs less than it gains: 65 536 positions, 1 list, 512 x 512 bf16: 723 to 1449 us
+// without, 82 with parts of 2048; 20 000 positions, 256 x 256 fp32: 544 and 55.  Above the line parts lose:
+// 8192 positions, 4 lists, 2048 x 1024: 56 us without, 74 to 222 with; 3000, 24 lists, 512 x 768: 18 and 37.
 int dw_part(int64_t pairs, int groups, int64_t n, int64_t k) {
   const int64_t tiles = up(n, 128) * up(k, 128);
-  if (tiles * groups >= 1024 || pairs < 512) return 0;
-  // as many parts as fill the chip twice, none shorter than 256 positions
-  const int64_t want = std::max<int64_t>(1, up(512, tiles));
-  return (int)(std::max<int64_t>(1, pairs / want / 256) * 256);
+  if (tiles * groups >= 512) return 0;
+  return (int)(std::max<int64_t>(1, pairs * tiles / 512 / 512) * 512);
 }
 
 int launch_product_dw(const ProductArgs& p, int dtype, float* scratch, hipStream_t st) {
   ProductArgs q = p;
-  q.part = p.pairs > 0 ? dw_part(p.pairs, p.groups, p.n, p.k) : 0;
-  if (q.part == 0) return launch_op<GRAD_W>(q, dtype, st);
-  q.out = scratch; q.ldo = p.k; q.stride = 0; q.out_dtype = RABITQ_F32;
+  q.part = dw_part(p.pairs, p.groups, p.n, p.k);
+  q.parts = scratch;
   const int rc = launch_op<GRAD_W>(q, dtype, st);
-  if (rc) return rc;
-  const int64_t elems = p.n * p.k;
-  const dim3 grid((unsigned)std::min<int64_t>(up(elems, 1024), 65535), (unsigned)std::min(p.groups, 65535));
-  if (p.out_dtype == RABITQ_F32) sum_parts_kernel<<<grid, 256, 0, st>>>(p, scratch, q.part, (float*)p.out);
-  else if (p.out_dtype == RABITQ_F16) sum_parts_kernel<<<grid, 256, 0, st>>>(p, scratch, q.part, (_Float16*)p.out);
-  else sum_parts_kernel<<<grid, 256, 0, st>>>(p, scratch, q.part, (__bf16*)p.out);
+  if (rc || q.part == 0) return rc;
+  const dim3 grid((unsigned)std::min<int64_t>(up(p.n * p.k, 1024), 65535), (unsigned)std::min(p.groups, 65535));
+  if (p.out_dtype == RABITQ_F32) sum_parts_kernel<<<grid, 256, 0, st>>>(q, (float*)p.out);
+  else if (p.out_dtype == RABITQ_F16) sum_parts_kernel<<<grid, 256, 0, st>>>(q, (_Float16*)p.out);
+  else sum_parts_kernel<<<grid, 256, 0, st>>>(q, (__bf16*)p.out);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }

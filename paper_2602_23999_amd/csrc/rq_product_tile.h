@@ -117,6 +117,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   extern __shared__ __align__(16) char smem[];
   int* row_pair = reinterpret_cast<int*>(smem + 2 * STAGE);  // [BI] pair of every row, or -1
   float* row_scale = reinterpret_cast<float*>(row_pair + BI);  // [BI] codes only
+  int* block_pairs = row_pair;                               // dw: [2][512] pairs of the positions
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
 
@@ -136,6 +137,8 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   int64_t i0, iend;
   uint32_t nc;  // length of the contraction, below 2^31: positions and pairs are 32-bit numbers
   void* out = p.out;
+  int out_dtype = p.out_dtype;
+  int64_t ldo = p.ldo, ostride = OP == GRAD_W ? p.stride : 0;
   if constexpr (OP == GRAD_W) {
     const int64_t it = (p.n + BI - 1) / BI;
     const int64_t unit = tile / it;  // a list, or (p.part > 0) a part of p.part positions of one
@@ -146,10 +149,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       s = span_of(p, g);
       const int64_t begin = s.begin + (unit - (s.begin / p.part + g)) * p.part;
       if (begin < s.begin || begin >= s.end) return;
+      if (s.end - s.begin > p.part) {  // one of several parts: its sums go to scratch
+        out = p.parts + unit * p.n * p.k;
+        out_dtype = RABITQ_F32;
+        ldo = p.k;
+        ostride = 0;
+      }
       s.end = min(s.end, begin + p.part);
       s.begin = begin;
-      g = 0;
-      out = static_cast<float*>(p.out) + unit * p.n * p.k;
     } else {
       g = (int)unit;
       s = span_of(p, g);
@@ -190,17 +197,30 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   const char* pb = nullptr;  // piece 0; the others lie whole lines behind it
   if constexpr (!TB) pb = b + ((j0 + line) * p.ldb + cb) * SZ;
   if constexpr (OP == GRAD_X) pb = b + (tid / PB * p.ldb + j0) * SZ;
-  // dw: the pairs of this thread's lines, a step ahead (the lines of both operands are the same)
-  constexpr int LP = TA ? NA : 1;
-  static_assert(!TA || BI == BJ);
-  int pairs_next[LP];
+  // dw: the pairs of this thread's lines, a step ahead (the lines of both operands are the same).  They come from a ring of two
+  // blocks of positions in LDS: loads of their own would have to arrive within a step, and all loads are waited for in order.
+  constexpr int LP = TA ? NA : 1, BLOCK = 512, FILL = BLOCK / NT;
+  static_assert(!TA || (BI == BJ && BLOCK % NT == 0));
+  int pairs_next[LP], block_next[FILL > 0 ? FILL : 1];
+  auto load_block = [&](uint32_t block) {
+    if constexpr (TA) {
+#pragma unroll
+      for (int f = 0; f < FILL; ++f) {
+        const uint32_t c = block * BLOCK + f * NT + tid;
+        block_next[f] = c < nc ? (int)pair_at(p, s.begin + c) : -1;
+      }
+    }
+  };
+  auto store_block = [&](uint32_t block) {
+    if constexpr (TA) {
+#pragma unroll
+      for (int f = 0; f < FILL; ++f) block_pairs[block % 2 * BLOCK + f * NT + tid] = block_next[f];
+    }
+  };
   auto find_pairs = [&](uint32_t c0) {
     if constexpr (TA) {
 #pragma unroll
-      for (int q = 0; q < NA; ++q) {
-        const uint32_t c = c0 + (uint32_t)(tid + q * NT) / PA;
-        pairs_next[q] = c < nc ? (int)pair_at(p, s.begin + c) : -1;
-      }
+      for (int q = 0; q < NA; ++q) pairs_next[q] = block_pairs[(c0 + (uint32_t)(tid + q * NT) / PA) % (2 * BLOCK)];
     }
   };
   // where piece q of the step at c0 lies, and how many of its elements exist (none or more than there are, as may be)
@@ -354,6 +374,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     }
   };
   if (nc > 0) {
+    if constexpr (TA) {
+      load_block(0);
+      store_block(0);
+      load_block(1);
+      store_block(1);
+      __syncthreads();
+    }
     find_pairs(0);
     fetch_all(0, 0);
     find_pairs(STEP);
@@ -370,12 +397,16 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     }
     int buf = 0;
     for (uint32_t c0 = 0; c0 < nc; c0 += STEP, buf ^= 1) {
+      // (the first step of block b: nobody looks at block b - 1 any more, and b + 1 is there)
+      const bool refill = TA && c0 != 0 && c0 % BLOCK == 0;
       multiply(sub0, buf, second, c0 + STEP, buf ^ 1);
+      if (refill) load_block(c0 / BLOCK + 1);
       multiply(sub1, buf, nothing, 0, 0);
       find_pairs(c0 + 2 * STEP);
       multiply(sub2, buf, nothing, 0, 0);
       stash(buf ^ 1);
       wait_and_barrier();
+      if (refill) store_block(c0 / BLOCK + 1);
       if constexpr (!FAST) fetch_regs(c0 + 2 * STEP);
       multiply(sub3, buf ^ 1, first, c0 + 2 * STEP, buf);
     }
@@ -386,9 +417,8 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   // rows go through LDS instead (its own part of it, as fp32, pieces of 16 bytes swizzled by the row) and out in whole rows of COLS.
   constexpr int COLS = FJ * 32, PIECES = COLS / 4;  // of a row: a power of two
   static_assert(32 * COLS * 4 * WI * WJ <= 2 * STAGE && (PIECES & (PIECES - 1)) == 0 && PIECES >= 8);
-  const int64_t ldo = p.ldo;
-  const int each = p.out_dtype == RABITQ_F32 ? 4 : 8;  // columns that a lane stores at once
-  const bool whole = (ldo | (OP == GRAD_W ? p.stride : 0)) % each == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
+  const int each = out_dtype == RABITQ_F32 ? 4 : 8;  // columns that a lane stores at once
+  const bool whole = (ldo | ostride) % each == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
   f32x4* mine = reinterpret_cast<f32x4*>(smem) + wave * (32 * PIECES);
   const int per_row = COLS / each, rows_at_once = 64 / per_row;
   const int col = lane % per_row * each;
@@ -417,7 +447,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       if (row < 0) continue;
       if (OP == GRAD_X && p.named && j == 0) p.named[row] = 1;
       if (j >= width) continue;
-      const int64_t at = (OP == GRAD_W ? (int64_t)g * p.stride : 0) + row * ldo + j;
+      const int64_t at = (int64_t)g * ostride + row * ldo + j;
       f32x4 lo = mine[r * PIECES + ((col >> 2) ^ (r & (PIECES - 1)))];
       f32x4 hi = lo;
       if (each == 8) hi = mine[r * PIECES + (((col >> 2) + 1) ^ (r & (PIECES - 1)))];
@@ -430,13 +460,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
         }
       }
       if (whole && j + each <= width) {
-        if (p.out_dtype == RABITQ_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = lo;
-        else if (p.out_dtype == RABITQ_F16) *reinterpret_cast<f16x8*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), f16x8);
+        if (out_dtype == RABITQ_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = lo;
+        else if (out_dtype == RABITQ_F16) *reinterpret_cast<f16x8*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), f16x8);
         else *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < each && j + e < width) store_as(out, p.out_dtype, at + e, e < 4 ? lo[e % 4] : hi[e % 4]);
+          if (e < each && j + e < width) store_as(out, out_dtype, at + e, e < 4 ? lo[e % 4] : hi[e % 4]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

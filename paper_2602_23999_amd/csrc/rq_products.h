@@ -39,7 +39,8 @@ struct ProductArgs {
   int out_dtype;
   int64_t tiles;              // of the launch
   int64_t chunk;              // neighbouring tiles that go to one XCD
-  int part;                   // dw: positions of a list that one workgroup sums up, or 0 (all): then out is [parts][n][k] fp32
+  int part;                   // dw: positions of a list that one workgroup sums up, or 0 (all)
+  float* parts;               // dw: [parts][n][k], the sums of lists of several parts
   uint8_t* named;             // dx of several probes: set to 1 for every pair a list names, or null
 };
 
@@ -93,9 +94,8 @@ __device__ __forceinline__ void store_as(void* out, int dtype, int64_t at, float
 // dtype: of the operands.  All sizes and pointers checked by the caller, work to do.
 int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st);
 int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st);
-// dw.  Few tiles of dw, or lists of very different lengths, would leave most of the chip idle while a long list is summed up by
-// one workgroup per tile, so the positions are cut into parts of dw_part(...) (0: not worth it), numbered as tiles are, whose
-// sums go to scratch and are added up in order.
+// dw.  Where there are few tiles of dw, a list is summed up in parts of dw_part(...) positions (0: not in parts), numbered as tiles are;
+// the sums of lists of several parts go to scratch and are added up in order.
 int dw_part(int64_t pairs, int groups, int64_t n, int64_t k);
 inline int64_t dw_parts(int64_t pairs, int groups, int part) { return pairs / part + groups; }
 int launch_product_dw(const ProductArgs& p, int dtype, float* scratch, hipStream_t st);
