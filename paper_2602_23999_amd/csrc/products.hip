@@ -72,9 +72,14 @@ static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
 static int launch_tiles(ProductArgs p, hipStream_t st) {
   const int64_t width = OP == FORWARD ? p.n : p.k;
-  p.chunk = std::max<int64_t>(1, up(width, BJ) / 8);
-  p.tiles = up(width, BJ) * (OP == GRAD_W ? up(p.n, BI) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups) : p.pair_off ? p.pairs / BI + p.groups : up(p.pairs, BI));
-  const int64_t grid = up(p.tiles, 8 * p.chunk) * 8 * p.chunk;
+  p.tiles_i = OP == GRAD_W ? up(p.n, BI) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups)
+                           : p.pair_off ? p.pairs / BI + p.groups : up(p.pairs, BI);
+  // strips of up to 8 tiles, evenly dealt out; shorter where that would be less than 16 for each XCD
+  const int64_t tiles_j = up(width, BJ), most = std::min<int64_t>(8, std::max<int64_t>(1, p.tiles_i * tiles_j / 128));
+  const int64_t strips = up(tiles_j, most), strip = up(tiles_j, strips);
+  p.strips = (uint32_t)strips;
+  p.strip = (uint32_t)strip;
+  const int64_t grid = up(p.tiles_i * strips, 8) * 8 * strip;
   if (grid > MAX_GRID / (64 * WI * WJ)) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;

@@ -125,13 +125,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   const int nj = OP == FORWARD ? (int)0 : p.k;
   const int64_t width = OP == FORWARD ? p.n : (int64_t)nj;  // of the output
   const int64_t jt = (width + BJ - 1) / BJ;
-  // Workgroups go to the 8 XCDs in turn; each XCD gets `chunk` neighbouring tiles of every 8 chunk, an eighth of the columns where
-  // there are that many: its share of b stays in its own L2 while the rows pass by, and no XCD gets more than a chunk of the work more
-  // than another.
-  const int64_t turn = blockIdx.x >> 3;
-  const int64_t id = (turn / p.chunk * 8 + (blockIdx.x & 7)) * p.chunk + turn % p.chunk;
-  if (id >= p.tiles) return;
-  const int64_t tile = id / jt, j0 = id % jt * BJ;
+  // Workgroups go to the 8 XCDs in turn.  An XCD gets strips of up to 8 neighbouring columns of tiles, whose share of a comes to its L2
+  // once.  (Strips of one row of tiles: 64 lists of 512 rows, 2048 x 2048 codes: 179 us; blocks of 4 x 8 tiles, which read
+  // least, 228: lists end inside them and XCDs run out of work at different times; an eighth of the columns each, 210.)
+  const uint32_t turn = blockIdx.x >> 3, strip = turn / p.strip * 8 + (blockIdx.x & 7);
+  const int64_t tile = strip / p.strips;
+  const int64_t j_tile = (int64_t)(strip % p.strips) * p.strip + turn % p.strip;
+  if (tile >= p.tiles_i || j_tile >= jt) return;
+  const int64_t j0 = j_tile * BJ;
   int g;
   Span s;
   int64_t i0, iend;

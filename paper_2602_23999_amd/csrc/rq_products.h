@@ -37,8 +37,8 @@ struct ProductArgs {
   int k, groups;
   Divisor probe;              // by the pairs per row of x
   int out_dtype;
-  int64_t tiles;              // of the launch
-  int64_t chunk;              // neighbouring tiles that go to one XCD
+  int64_t tiles_i;            // of the launch, along the rows
+  uint32_t strip, strips;     // neighbouring tiles of a row of tiles that go to one XCD, and how many such strips a row has
   int part;                   // dw: positions of a list that one workgroup sums up, or 0 (all)
   float* parts;               // dw: [parts][n][k], the sums of lists of several parts
   uint8_t* named;             // dx of several probes: set to 1 for every pair a list names, or null
