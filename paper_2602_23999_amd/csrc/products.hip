@@ -86,9 +86,12 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
   }
   const size_t lds = 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int) : BI * (sizeof(int) + sizeof(float)));
   auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, FAST>;
-  static const hipError_t granted =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  RQ_HIP(granted);
+  if (p.check_only) return RABITQ_OK;
+  static bool granted = false;  // more LDS than a launch gets unasked
+  if (!granted) {
+    RQ_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    granted = true;
+  }
   kernel<<<(unsigned)grid, 64 * WI * WJ, lds, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;

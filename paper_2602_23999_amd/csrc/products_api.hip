@@ -41,6 +41,7 @@ int check_lists(const char* call, const rabitq_lists* l) {
   if (l->pairs % l->nprobe != 0) return bad(call, "pairs must be a multiple of nprobe");
   if (l->n < 1 || l->n > MAX_WIDTH || l->k < 1 || l->k > MAX_WIDTH) return bad(call, "n and k must lie in 1 .. 2^20");
   if (!l->pair_off) return bad(call, "null pointer");
+  if (!aligned(l->pair_off, 4) || !aligned(l->pair_ids, 4)) return bad(call, "pointer not aligned to its type");
   return RABITQ_OK;
 }
 
@@ -106,6 +107,9 @@ int rabitq_grouped_matmul_dx(const rabitq_lists* l, int32_t dtype, const void* d
     p.named = static_cast<uint8_t*>(scratch);
     float* parts = reinterpret_cast<float*>(p.named + named_bytes(l->pairs));
     p.out = parts; p.ldo = l->k; p.out_dtype = RABITQ_F32;
+    p.check_only = true;  // (nothing is written by a call that is refused)
+    if ((rc = launch_product_dx(p, dtype, st))) return rc;
+    p.check_only = false;
     if ((rc = launch_clear_bytes(p.named, l->pairs, st))) return rc;
     if ((rc = launch_product_dx(p, dtype, st))) return rc;
     return launch_sum_named(parts, p.named, l->pairs / l->nprobe, l->nprobe, l->k, dx, dtype, ldx, st);

@@ -37,6 +37,7 @@ struct ProductArgs {
   int k, groups;
   Divisor probe;              // by the pairs per row of x
   int out_dtype;
+  bool check_only;            // say whether the launch would be refused, and launch nothing
   int64_t tiles_i;            // of the launch, along the rows
   uint32_t strip, strips;     // neighbouring tiles of a row of tiles that go to one XCD, and how many such strips a row has
   int part;                   // dw: positions of a list that one workgroup sums up, or 0 (all)

@@ -40,19 +40,22 @@ def pairs_of(off, ids, pairs):
     return out
 
 
-def _by_list(off, ids, pairs):
+def _by_list(off, ids, pairs, device="cpu"):
     lists = {}
-    for g, p in pairs_of(off, ids, pairs):
+    for g, p in pairs_of(off.tolist(), None if ids is None else ids.tolist(), pairs):
         lists.setdefault(g, []).append(p)
-    return {g: torch.tensor(p) for g, p in lists.items()}
+    return {g: torch.tensor(p, device=device) for g, p in lists.items()}
+
+
+# The 64-bit products run where x and w lie: on the CPU, or, for sizes that take it too long, as the library's fp64 products.
 
 
 def forward64(x, w, off, ids, nprobe):
     """(out, sum of |products|, named) in 64 bits."""
     x, w = x.double(), w.double()
     pairs = x.shape[0] * nprobe
-    y, mag, named = torch.zeros(pairs, w.shape[1]).double(), torch.zeros(pairs, w.shape[1]).double(), torch.zeros(pairs).bool()
-    for g, p in _by_list(off, ids, pairs).items():
+    y, mag, named = x.new_zeros(pairs, w.shape[1]), x.new_zeros(pairs, w.shape[1]), torch.zeros(pairs, device=x.device).bool()
+    for g, p in _by_list(off, ids, pairs, x.device).items():
         y[p], mag[p], named[p] = x[p // nprobe] @ w[g].t(), x[p // nprobe].abs() @ w[g].abs().t(), True
     return y, mag, named
 
@@ -60,8 +63,8 @@ def forward64(x, w, off, ids, nprobe):
 def dx64(dy, w, off, ids, nprobe):
     dy, w = dy.double(), w.double()
     pairs = dy.shape[0]
-    d, mag, named = (torch.zeros(pairs, w.shape[2]).double(), torch.zeros(pairs, w.shape[2]).double(), torch.zeros(pairs).bool())
-    for g, p in _by_list(off, ids, pairs).items():
+    d, mag, named = dy.new_zeros(pairs, w.shape[2]), dy.new_zeros(pairs, w.shape[2]), torch.zeros(pairs, device=dy.device).bool()
+    for g, p in _by_list(off, ids, pairs, dy.device).items():
         d[p], mag[p], named[p] = dy[p] @ w[g], dy[p].abs() @ w[g].abs(), True
     rows = lambda t: t.reshape(pairs // nprobe, nprobe, -1)
     return rows(d).sum(1), rows(mag).sum(1), named.reshape(-1, nprobe).any(1)
@@ -70,8 +73,8 @@ def dx64(dy, w, off, ids, nprobe):
 def dw64(dy, x, off, ids, nprobe):
     dy, x = dy.double(), x.double()
     groups = len(off) - 1
-    d, mag = torch.zeros(groups, dy.shape[1], x.shape[1]).double(), torch.zeros(groups, dy.shape[1], x.shape[1]).double()
-    for g, p in _by_list(off, ids, dy.shape[0]).items():
+    d, mag = dy.new_zeros(groups, dy.shape[1], x.shape[1]), dy.new_zeros(groups, dy.shape[1], x.shape[1])
+    for g, p in _by_list(off, ids, dy.shape[0], dy.device).items():
         d[g], mag[g] = dy[p].t() @ x[p // nprobe], dy[p].abs().t() @ x[p // nprobe].abs()
     return d, mag
 
@@ -84,7 +87,7 @@ def assert_sums(got, want, mag, terms, dtype, what=""):
     """got is an fp32 sum of `terms` products, rounded once to dtype.  Products of two fp32 numbers are rounded (2^-24 of each),
     and every addition, in whatever order, may lose an ulp (2^-23, where the matrix unit does not round to nearest) of a partial sum that is no
     larger than the sum of magnitudes: (terms + 1) 2^-23 mag in all; then half a step of dtype, and of its smallest numbers."""
-    err = (got.double().cpu() - want).abs()
+    err = (got.double().to(want.device) - want).abs()
     sums = (terms + 1) * 2.0 ** -23 * mag
     tol = sums + half_step(dtype) * (want.abs() + sums) + torch.finfo(dtype).tiny * torch.finfo(dtype).eps
     worst = (err - tol).max().item() if err.numel() else -1.0
@@ -110,7 +113,7 @@ def assert_scaled(got, want, dtype, what=""):
     """got is an exact whole number converted to fp32, multiplied twice and rounded to dtype: three roundings of 2^-24 (their
     product's second order in the 4), and half a step of dtype; where a scale is small, half a step of the smallest numbers
     each time."""
-    err = (got.double().cpu() - want).abs()
+    err = (got.double().to(want.device) - want).abs()
     tol = 4 * 2.0 ** -24 * want.abs() + 1.01 * half_step(dtype) * want.abs() + torch.finfo(dtype).tiny * torch.finfo(dtype).eps
     worst = (err - tol).max().item() if err.numel() else -1.0
     assert not torch.isnan(err).any() and worst <= 0, f"{what}: off by {err.max().item():.3e}, {worst:.3e} more than allowed"
@@ -119,7 +122,6 @@ def assert_scaled(got, want, dtype, what=""):
 def grouped_i8_64(x, sx, w, sw, off, ids, nprobe):
     """(out, named): whole-number sums, exact in 64 bits, times the scales."""
     y, _, named = forward64(x, w, off, ids, nprobe)
-    pairs = y.shape[0]
-    for g, p in _by_list(off, ids, pairs).items():
+    for g, p in _by_list(off, ids, y.shape[0], y.device).items():
         y[p] *= sx.double()[p // nprobe][:, None] * sw.double()[g][None, :]
     return y, named

@@ -184,6 +184,76 @@ def test_quantize_rows_near_ties(dtype):
     assert torch.equal(scale.cpu(), want_scale) and torch.equal(codes.cpu(), want)
 
 
+# ---- larger tiles and long contractions ----------------------------------------------
+
+def _even(dtype):
+    """Elements of 16 bytes."""
+    return 16 // torch.empty(0, dtype=dtype).element_size()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,groups,odd", [(1200, 8, 0), (1200, 8, 1), (4500, 2, 0)])
+def test_large_products(rows, groups, odd, dtype):
+    # 128 x 128 tiles (with rows that do not start at multiples of 16 bytes too) and 256 x 256 tiles: lists that end inside a
+    # tile, columns that do, a contraction that ends inside a step
+    wide, short = 4096 + 3 * _even(dtype) + odd, 264 + _even(dtype) + odd
+    off, ids = lists_from(probes_of(rows, rows, 1, groups, 0, 0.02), groups)
+    lists = off.cuda(), ids.cuda(), 1
+    x, w = numbers(1, (rows, short), dtype).cuda(), numbers(2, (groups, wide, short), dtype).cuda()
+    want, mag, named = forward64(x, w, off, ids, 1)
+    got = rabitq.grouped_matmul(x, w, *lists, out=torch.full((rows, wide), 7.0, dtype=dtype, device="cuda"))
+    assert_sums(got[named], want[named], mag[named], short, dtype)
+    assert (got[~named] == 7.0).all()
+    w = numbers(3, (groups, short, wide), dtype).cuda()
+    want, mag, named = dx64(x, w, off, ids, 1)
+    got = rabitq.grouped_matmul_dx(x, w, *lists, out=torch.full((rows, wide), 7.0, dtype=dtype, device="cuda"))
+    assert_sums(got[named], want[named], mag[named], short, dtype)
+    assert (got[~named] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("nq,nprobe,groups,n,k", [
+    (500, 2, 4, 2048, 2056),    # 256 x 256 tiles
+    (900, 1, 8, 1000, 1032),    # 128 x 128 tiles
+    (400, 3, 8, 1001, 1029),    # the same, rows that do not start at multiples of 16 bytes
+    (5000, 1, 2, 2048, 2048),   # lists longer than what is known of their pairs at a time
+    (70000, 1, 1, 264, 256),    # one list in parts of 2048 and more
+    (30000, 2, 3, 130, 72),
+    (9000, 1, 40, 24, 40),      # most lists in one part, some in two
+], ids=str)
+def test_large_dw(nq, nprobe, groups, n, k, dtype):
+    probes = probes_of(7, nq, nprobe, groups, 0, 0.01)
+    if groups > 8:
+        probes = torch.where(torch.rand(probes.shape, generator=torch.Generator().manual_seed(8)) < 0.2, 5, probes)  # a long list
+    off, ids = lists_from(probes, groups)
+    x, dy = numbers(1, (nq, k), dtype).cuda(), numbers(2, (nq * nprobe, n), dtype).cuda()
+    want, mag = dw64(dy, x, off, ids, nprobe)
+    got = rabitq.grouped_matmul_dw(dy, x, off.cuda(), ids.cuda(), nprobe)
+    assert_sums(got, want, mag, int((off[1:] - off[:-1]).max()), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("m,n,k", [(4200, 4100, 528), (1100, 8200, 272), (1030, 8195, 515), (48, 5000, 3000), (40, 70000, 100)])
+def test_large_matmul_i8(m, n, k, dtype):
+    g = torch.Generator().manual_seed(m)
+    a, b = (torch.randint(-128, 128, (r, k), generator=g).to(torch.int8).cuda() for r in (m, n))
+    sa, sb = (torch.exp(torch.randn(r, generator=g)).cuda() for r in (m, n))
+    assert_scaled(rabitq.matmul_i8(a, sa, b, sb, dtype), i8_64(a, sa, b, sb), dtype)
+
+
+@pytest.mark.parametrize("rows,nprobe,groups,n,k", [(2300, 2, 2, 4112, 528), (700, 2, 8, 4104, 528), (3000, 3, 5, 515, 260)])
+def test_large_grouped_matmul_i8(rows, nprobe, groups, n, k):
+    g = torch.Generator().manual_seed(rows)
+    off, ids = lists_from(probes_of(rows, rows, nprobe, groups, 0, 0.02), groups)
+    x, w = (torch.randint(-128, 128, s, generator=g).to(torch.int8).cuda() for s in ((rows, k), (groups, n, k)))
+    sx, sw = torch.rand(rows, generator=g).cuda(), torch.rand(groups, n, generator=g).cuda()
+    want, named = grouped_i8_64(x, sx, w, sw, off, ids, nprobe)
+    got = rabitq.grouped_matmul_i8(x, sx, w, sw, off.cuda(), ids.cuda(), nprobe, torch.float32,
+                                   torch.full((rows * nprobe, n), 7.0, device="cuda"))
+    assert_scaled(got[named], want[named], torch.float32)
+    assert (got[~named] == 7.0).all()
+
+
 # ---- layouts ------------------------------------------------------------------------
 
 def _strided(t, pad, shift):

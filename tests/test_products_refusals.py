@@ -38,7 +38,8 @@ def _calls():
 
 
 BAD_LISTS = [dict(groups=0), dict(groups=-1), dict(nprobe=0), dict(pairs=-2), dict(pairs=7), dict(pairs=1 << 31),
-             dict(n=0), dict(k=0), dict(n=(1 << 20) + 1), dict(k=(1 << 20) + 1), dict(off=None)]
+             dict(n=0), dict(k=0), dict(n=(1 << 20) + 1), dict(k=(1 << 20) + 1), dict(off=None), dict(off=P + 2),
+             dict(ids=P + 1)]
 
 
 @pytest.mark.parametrize("name", ["fwd", "dx", "dw", "gi8"])
@@ -75,6 +76,20 @@ def test_k_of_codes_by_list_is_bounded():
     k = 131072
     assert _calls()["gi8"](ls=_ls(k=k), ldx=k, ldw=k, stride=8 * k) == -1
     assert b"131071" in rabitq.load_library().rabitq_last_error()
+
+
+def test_more_work_than_a_launch_holds():
+    big = (1 << 31) - 1
+    c = _calls()
+    assert c["i8"](m=big, n=big, ldo=big) == -1
+    assert b"too many tiles" in rabitq.load_library().rabitq_last_error()
+    ls = dict(pairs=big - 1, n=1 << 20, k=16)
+    assert c["fwd"](ls=_ls(**ls), ldo=1 << 20, stride=1 << 24) == -1
+    assert c["dx"](ls=_ls(pairs=big - 1, k=1 << 20), ldw=1 << 20, ldo=1 << 20, stride=1 << 23) == -1
+    wide = 1 << 20
+    assert c["dw"](ls=_ls(groups=64, n=wide, k=wide), ldd=wide, ldx=wide, ldo=wide, stride=1 << 40) == -1
+    assert c["quant"](rows=1 << 40, k=8192, ldx=8192, ldc=8192) == -1
+    assert b"too many rows" in rabitq.load_library().rabitq_last_error()
 
 
 def test_null_lists():
