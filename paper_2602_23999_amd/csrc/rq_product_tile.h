@@ -62,7 +62,7 @@ __device__ __forceinline__ int j_of_row(int m) { return 16 * ((m >> 2) & 1) + 4 
 // 16 bytes per lane from memory to LDS without registers: lane l's go to lds + 16 l.  Not waited for by the compiler: the kernel
 // waits for all of them in front of the barrier behind which they are read.
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
 // (As builtins and not in the asm, so that the compiler's own count of LDS reads in flight starts again from none.)
 __device__ __forceinline__ void wait_and_barrier() {
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   auto multiply = [&](auto sub_c, int next_buf, auto request_c, uint32_t c2, int buf2) {
     constexpr int sub = decltype(sub_c)::value, set = sub & 1;
     const char* st = smem + next_buf * STAGE;
-    constexpr int READS = FI + FJ, ROWS = FI >= 2 ? FI / 2 : 1;  // rows of products that reads are dealt out among: the first half
+    constexpr int READS = FI + FJ, ROWS = FI >= 2 ? FI - 1 : 1;  // rows of products that reads are dealt out among: all but the last
 #pragma unroll
     for (int x = 0; x < FI; ++x) {
 #pragma unroll

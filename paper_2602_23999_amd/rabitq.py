@@ -377,56 +377,60 @@ class Index:
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
-def _here(t: torch.Tensor, dtype, dims: int, what: str):
-    """A tensor of the current device with `dims` dimensions, whose last one is contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+def _operand(t, dtype, dims: int, what: str, dev: int):
+    """(address, shape, row stride, matrix stride) of a tensor of device `dev` with `dims` dimensions, whose last one is
+    contiguous.  (Written for few calls into torch: beside kernels of a few microseconds the checks count.)"""
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev or dev < 0:
         raise RabitqError(f"{what}: expected a tensor on the current CUDA device")
     if t.dtype is not dtype or t.dim() != dims:
         raise RabitqError(f"{what}: expected {dims} dimensions of {dtype}, got {t.dim()} of {t.dtype}")
     if t.requires_grad and torch.is_grad_enabled():
         raise RabitqError(f"{what} requires a gradient, which this call does not record: pass it detached or under "
                           "torch.no_grad()")
-    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
+    shape = t.shape
+    if t.is_contiguous():
+        ld = shape[-1]
+        return t.data_ptr(), shape, ld, ld * shape[1] if dims == 3 else 0
+    if t.stride(-1) != 1 and shape[-1] > 1 and t.numel():
         raise RabitqError(f"{what}: the last dimension must be contiguous")
-    return t
+    # the stride of a dimension of one says nothing
+    ld = t.stride(-2) if dims > 1 and shape[-2] > 1 else shape[-1]
+    return t.data_ptr(), shape, ld, (t.stride(0) if shape[0] > 1 else ld * shape[1]) if dims == 3 else 0
 
 
-def _current_stream(t: torch.Tensor) -> int:
-    """_stream() for a tensor that _here has seen; a third of its time, which counts beside kernels of a few microseconds."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+def _current_device(t) -> int:
+    """The current device if t lies there (and -1 if t lies on the host or is no tensor, which _operand refuses)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        return -1
+    return torch._C._cuda_getDevice()
 
 
-def _ld(t: torch.Tensor) -> int:
-    """The row stride; of a single row, whose stride says nothing, the row's length."""
-    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
-
-
-def _matrix_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else _ld(t) * t.shape[1]
-
-
-def _float_type(t: torch.Tensor, what: str):
+def _float_type(t, what: str):
     if not isinstance(t, torch.Tensor) or t.dtype not in DTYPES:
         raise RabitqError(f"{what}: expected float32, float16 or bfloat16")
     return t.dtype
 
 
-def _output(out, shape, dtype, device, what="out"):
+def _output(out, shape, dtype, like, dev: int, what="out"):
+    """(tensor, address, row stride, matrix stride) of the caller's output, or of a new one on the device of `like`."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if _here(out, dtype, len(shape), what).shape != shape:
-        raise RabitqError(f"{what}: expected the shape {tuple(shape)}, got {tuple(out.shape)}")
-    return out
+        out = like.new_empty(shape, dtype=dtype)
+    ptr, have, ld, stride = _operand(out, dtype, len(shape), what, dev)
+    if have != shape:
+        raise RabitqError(f"{what}: expected the shape {tuple(shape)}, got {tuple(have)}")
+    return out, ptr, ld, stride
 
 
-def _lists_of(groups: int, n: int, k: int, pairs: int, nprobe: int, pair_off, pair_ids) -> "_Lists":
-    if _here(pair_off, torch.int32, 1, "pair_off").shape[0] != groups + 1:
-        raise RabitqError(f"pair_off must hold {groups + 1} offsets, got {pair_off.shape[0]}")
-    if pair_ids is None:
-        return _Lists(groups, nprobe, pairs, n, k, pair_off.data_ptr(), None)
-    if _here(pair_ids, torch.int32, 1, "pair_ids").shape[0] != pairs:
-        raise RabitqError(f"pair_ids must hold {pairs} pairs, got {pair_ids.shape[0]}")
-    return _Lists(groups, nprobe, pairs, n, k, pair_off.data_ptr(), pair_ids.data_ptr())
+def _vector(t, dtype, shape, what: str, dev: int) -> int:
+    ptr, have, _, _ = _operand(t, dtype, len(shape), what, dev)
+    if have != shape or not t.is_contiguous():
+        raise RabitqError(f"{what}: expected a contiguous tensor of the shape {tuple(shape)}, got {tuple(have)}")
+    return ptr
+
+
+def _lists_of(groups: int, n: int, k: int, pairs: int, nprobe: int, pair_off, pair_ids, dev: int) -> "_Lists":
+    return _Lists(groups, nprobe, pairs, n, k, _vector(pair_off, torch.int32, (groups + 1,), "pair_off", dev),
+                  None if pair_ids is None else _vector(pair_ids, torch.int32, (pairs,), "pair_ids", dev))
 
 
 def _nprobe(nprobe) -> int:
@@ -435,118 +439,113 @@ def _nprobe(nprobe) -> int:
     return int(nprobe)
 
 
-def _scales(t, shape, what):
-    if _here(t, torch.float32, len(shape), what).shape != shape or not t.is_contiguous():
-        raise RabitqError(f"{what}: expected a contiguous tensor of the shape {tuple(shape)}")
-    return t.data_ptr()
-
-
-def _scratch(n: int, device):
+def _scratch(n: int, like):
     if n < 0:
         _check(int(n))
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    return like.new_empty(n, dtype=torch.uint8) if n else None
 
 
 def grouped_matmul(x, w, pair_off, pair_ids=None, nprobe: int = 1, out=None):
     """rabitq_grouped_matmul: out[p] = w[list of p] @ x[p // nprobe] for the pairs of pair_off / pair_ids
     (Index.build_probe_lists).  x [nq, k] and w [lists, n, k] of float32, float16 or bfloat16; returns out [nq * nprobe, n].
     Rows of pairs that no list names are left as they were (in a new output: undefined)."""
-    dt = _float_type(x, "x")
-    _here(x, dt, 2, "x"), _here(w, dt, 3, "w")
-    (nq, k), (g, n, _), nprobe = x.shape, w.shape, _nprobe(nprobe)
-    if w.shape[2] != k:
-        raise RabitqError(f"rows of x have {k} elements, those of w {w.shape[2]}")
-    ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids)
-    out = _output(out, (nq * nprobe, n), dt, x.device)
-    _check(load_library().rabitq_grouped_matmul(C.byref(ls), DTYPES[dt], x.data_ptr(), _ld(x), w.data_ptr(), _ld(w),
-                                                _matrix_stride(w), out.data_ptr(), _ld(out), _current_stream(out)))
+    dt, dev, nprobe = _float_type(x, "x"), _current_device(x), _nprobe(nprobe)
+    px, (nq, k), ldx, _ = _operand(x, dt, 2, "x", dev)
+    pw, (g, n, kw), ldw, stride_w = _operand(w, dt, 3, "w", dev)
+    if kw != k:
+        raise RabitqError(f"rows of x have {k} elements, those of w {kw}")
+    ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids, dev)
+    out, po, ldo, _ = _output(out, (nq * nprobe, n), dt, x, dev)
+    _check(load_library().rabitq_grouped_matmul(C.byref(ls), DTYPES[dt], px, ldx, pw, ldw, stride_w, po, ldo,
+                                                torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
 def grouped_matmul_dx(dout, w, pair_off, pair_ids=None, nprobe: int = 1, out=None):
     """rabitq_grouped_matmul_dx: the gradient of grouped_matmul with respect to x, [nq, k], from dout [nq * nprobe, n]; the
     sum over a row's nprobe pairs is in it.  Rows none of whose pairs a list names are left as they were."""
-    dt, nprobe = _float_type(dout, "dout"), _nprobe(nprobe)
-    _here(dout, dt, 2, "dout"), _here(w, dt, 3, "w")
-    pairs, (g, n, k) = dout.shape[0], w.shape
-    if dout.shape[1] != n:
-        raise RabitqError(f"rows of dout have {dout.shape[1]} elements, matrices of w {n} rows")
+    dt, dev, nprobe = _float_type(dout, "dout"), _current_device(dout), _nprobe(nprobe)
+    pd, (pairs, nd), ldd, _ = _operand(dout, dt, 2, "dout", dev)
+    pw, (g, n, k), ldw, stride_w = _operand(w, dt, 3, "w", dev)
+    if nd != n:
+        raise RabitqError(f"rows of dout have {nd} elements, matrices of w {n} rows")
     if pairs % nprobe:
         raise RabitqError("dout must have nprobe rows per row of x")
-    ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids)
-    out = _output(out, (pairs // nprobe, k), dt, dout.device)
+    ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids, dev)
+    out, po, ldo, _ = _output(out, (pairs // nprobe, k), dt, dout, dev)
     lib = load_library()
-    scratch = _scratch(lib.rabitq_grouped_dx_scratch_bytes(C.byref(ls)), dout.device)
-    _check(lib.rabitq_grouped_matmul_dx(C.byref(ls), DTYPES[dt], dout.data_ptr(), _ld(dout), w.data_ptr(), _ld(w),
-                                        _matrix_stride(w), out.data_ptr(), _ld(out),
+    scratch = _scratch(lib.rabitq_grouped_dx_scratch_bytes(C.byref(ls)), dout)
+    _check(lib.rabitq_grouped_matmul_dx(C.byref(ls), DTYPES[dt], pd, ldd, pw, ldw, stride_w, po, ldo,
                                         None if scratch is None else scratch.data_ptr(),
-                                        _current_stream(out)))
+                                        torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
 def grouped_matmul_dw(dout, x, pair_off, pair_ids=None, nprobe: int = 1, out=None):
     """rabitq_grouped_matmul_dw: the gradient of grouped_matmul with respect to w, [lists, n, k], from dout [nq * nprobe, n]
     and x [nq, k].  Zeros for lists without pairs."""
-    dt, nprobe = _float_type(dout, "dout"), _nprobe(nprobe)
-    _here(dout, dt, 2, "dout"), _here(x, dt, 2, "x")
-    (pairs, n), (nq, k) = dout.shape, x.shape
+    dt, dev, nprobe = _float_type(dout, "dout"), _current_device(dout), _nprobe(nprobe)
+    pd, (pairs, n), ldd, _ = _operand(dout, dt, 2, "dout", dev)
+    px, (nq, k), ldx, _ = _operand(x, dt, 2, "x", dev)
     if pairs != nq * nprobe:
         raise RabitqError(f"dout must have {nq * nprobe} rows, got {pairs}")
-    _here(pair_off, torch.int32, 1, "pair_off")
-    g = pair_off.shape[0] - 1
-    ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids)
-    out = _output(out, (g, n, k), dt, dout.device)
+    g = _operand(pair_off, torch.int32, 1, "pair_off", dev)[1][0] - 1
+    ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids, dev)
+    out, po, ldo, stride = _output(out, (g, n, k), dt, dout, dev)
     lib = load_library()
-    scratch = _scratch(lib.rabitq_grouped_dw_scratch_bytes(C.byref(ls)), dout.device)
-    _check(lib.rabitq_grouped_matmul_dw(C.byref(ls), DTYPES[dt], dout.data_ptr(), _ld(dout), x.data_ptr(), _ld(x),
-                                        out.data_ptr(), _ld(out), _matrix_stride(out),
+    scratch = _scratch(lib.rabitq_grouped_dw_scratch_bytes(C.byref(ls)), dout)
+    _check(lib.rabitq_grouped_matmul_dw(C.byref(ls), DTYPES[dt], pd, ldd, px, ldx, po, ldo, stride,
                                         None if scratch is None else scratch.data_ptr(),
-                                        _current_stream(out)))
+                                        torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
 def quantize_rows(x, codes=None, scale=None):
     """rabitq_quantize_rows: x [rows, k] of float32, float16 or bfloat16 -> int8 codes [rows, k] and float32 scale [rows], with
     x about codes * scale[:, None]."""
-    dt = _float_type(x, "x")
-    _here(x, dt, 2, "x")
-    rows, k = x.shape
-    codes = _output(codes, (rows, k), torch.int8, x.device, "codes")
-    scale = _output(scale, (rows,), torch.float32, x.device, "scale")
-    _check(load_library().rabitq_quantize_rows(x.data_ptr(), DTYPES[dt], _ld(x), rows, k, codes.data_ptr(), _ld(codes),
-                                               _scales(scale, (rows,), "scale"), _current_stream(codes)))
+    dt, dev = _float_type(x, "x"), _current_device(x)
+    px, (rows, k), ldx, _ = _operand(x, dt, 2, "x", dev)
+    codes, pc, ldc, _ = _output(codes, (rows, k), torch.int8, x, dev, "codes")
+    if scale is None:
+        scale = x.new_empty(rows, dtype=torch.float32)
+    _check(load_library().rabitq_quantize_rows(px, DTYPES[dt], ldx, rows, k, pc, ldc,
+                                               _vector(scale, torch.float32, (rows,), "scale", dev),
+                                               torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale
 
 
 def matmul_i8(a, scale_a, b, scale_b, out_dtype=torch.float32, out=None):
     """rabitq_matmul_i8: out[i, j] = scale_a[i] * scale_b[j] * sum_t a[i, t] * b[j, t] for int8 a [m, k] and b [n, k]."""
-    _here(a, torch.int8, 2, "a"), _here(b, torch.int8, 2, "b")
-    (m, k), n = a.shape, b.shape[0]
-    if b.shape[1] != k:
-        raise RabitqError(f"rows of a have {k} elements, those of b {b.shape[1]}")
+    dev = _current_device(a)
+    pa, (m, k), lda, _ = _operand(a, torch.int8, 2, "a", dev)
+    pb, (n, kb), ldb, _ = _operand(b, torch.int8, 2, "b", dev)
+    if kb != k:
+        raise RabitqError(f"rows of a have {k} elements, those of b {kb}")
     if out_dtype not in DTYPES:
         raise RabitqError("out_dtype must be float32, float16 or bfloat16")
-    out = _output(out, (m, n), out_dtype, a.device)
-    _check(load_library().rabitq_matmul_i8(a.data_ptr(), _ld(a), _scales(scale_a, (m,), "scale_a"), b.data_ptr(), _ld(b),
-                                           _scales(scale_b, (n,), "scale_b"), m, n, k, out.data_ptr(), DTYPES[out_dtype],
-                                           _ld(out), _current_stream(out)))
+    out, po, ldo, _ = _output(out, (m, n), out_dtype, a, dev)
+    _check(load_library().rabitq_matmul_i8(pa, lda, _vector(scale_a, torch.float32, (m,), "scale_a", dev), pb, ldb,
+                                           _vector(scale_b, torch.float32, (n,), "scale_b", dev), m, n, k, po,
+                                           DTYPES[out_dtype], ldo, torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
 def grouped_matmul_i8(x, scale_x, w, scale_w, pair_off, pair_ids=None, nprobe: int = 1, out_dtype=torch.float32, out=None):
     """rabitq_grouped_matmul_i8: grouped_matmul on codes, x [nq, k] with scale_x [nq] and w [lists, n, k] with scale_w
     [lists, n]."""
-    _here(x, torch.int8, 2, "x"), _here(w, torch.int8, 3, "w")
-    (nq, k), (g, n, _), nprobe = x.shape, w.shape, _nprobe(nprobe)
-    if w.shape[2] != k:
-        raise RabitqError(f"rows of x have {k} elements, those of w {w.shape[2]}")
+    dev, nprobe = _current_device(x), _nprobe(nprobe)
+    px, (nq, k), ldx, _ = _operand(x, torch.int8, 2, "x", dev)
+    pw, (g, n, kw), ldw, stride_w = _operand(w, torch.int8, 3, "w", dev)
+    if kw != k:
+        raise RabitqError(f"rows of x have {k} elements, those of w {kw}")
     if out_dtype not in DTYPES:
         raise RabitqError("out_dtype must be float32, float16 or bfloat16")
-    ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids)
-    out = _output(out, (nq * nprobe, n), out_dtype, x.device)
+    ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids, dev)
+    out, po, ldo, _ = _output(out, (nq * nprobe, n), out_dtype, x, dev)
     _check(load_library().rabitq_grouped_matmul_i8(
-        C.byref(ls), x.data_ptr(), _ld(x), _scales(scale_x, (nq,), "scale_x"), w.data_ptr(), _ld(w), _matrix_stride(w),
-        _scales(scale_w, (g, n), "scale_w"), out.data_ptr(), DTYPES[out_dtype], _ld(out), _current_stream(out)))
+        C.byref(ls), px, ldx, _vector(scale_x, torch.float32, (nq,), "scale_x", dev), pw, ldw, stride_w,
+        _vector(scale_w, torch.float32, (g, n), "scale_w", dev), po, DTYPES[out_dtype], ldo,
+        torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
