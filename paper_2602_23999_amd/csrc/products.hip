@@ -84,7 +84,7 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
-  const size_t lds = 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int) : BI * (sizeof(int) + sizeof(float)));
+  const size_t lds = 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int2) : BI * (sizeof(int) + sizeof(float)));
   auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, FAST>;
   if (p.check_only) return RABITQ_OK;
   static bool granted = false;  // more LDS than a launch gets unasked
@@ -97,12 +97,15 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
   return RABITQ_OK;
 }
 
-// Rows of whole 16-byte pieces at multiples of 16 bytes: the pieces can go to LDS without registers.
+// Rows of whole 16-byte pieces at multiples of 16 bytes: the pieces can go to LDS without registers.  The kernel's 32-bit offsets
+// have to reach every row of a from the first one (dw: each row's length), and 256 rows of b (as many as a tile or a step has).
 static bool fast_rows(const ProductArgs& p, int op, int dtype) {
-  const int64_t sz = dtype_bytes(dtype), per = 16 / sz;
-  const int64_t in_a = op == FORWARD ? p.k : p.n;  // elements of a row of each operand
+  const int64_t sz = dtype_bytes(dtype), per = 16 / sz, reach = (int64_t)1 << 32;
+  const int64_t in_a = op == FORWARD ? p.k : p.n;  // elements of a row
+  const int64_t rows_a = op == GRAD_W ? 1 : p.rows_a;
   return in_a % per == 0 && p.k % per == 0 && p.lda % per == 0 && p.ldb % per == 0 && (op == GRAD_W || p.stride % per == 0 || p.groups == 1) &&
-         reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && reinterpret_cast<uintptr_t>(p.b) % 16 == 0;
+         reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && reinterpret_cast<uintptr_t>(p.b) % 16 == 0 &&
+         rows_a * p.lda * sz < reach && 256 * p.ldb * sz < reach;
 }
 
 // Whether the forward product goes to the kernel that streams the matrices.  It reads them once per 16 rows, the tile kernel once per 128 or

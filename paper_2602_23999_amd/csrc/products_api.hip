@@ -71,7 +71,7 @@ int rabitq_grouped_matmul(const rabitq_lists* l, int32_t dtype, const void* x, i
     const int64_t sz = dtype_bytes(dtype);
     if (!aligned(x, sz) || !aligned(w, sz) || !aligned(out, sz)) return bad(call, "pointer not aligned to its type");
     ProductArgs p = args_of(l);
-    p.a = x; p.lda = ldx; p.b = w; p.ldb = ldw; p.stride = stride_w; p.out = out; p.ldo = ldo; p.out_dtype = dtype;
+    p.a = x; p.lda = ldx; p.rows_a = l->pairs / l->nprobe; p.b = w; p.ldb = ldw; p.stride = stride_w; p.out = out; p.ldo = ldo; p.out_dtype = dtype;
     return launch_product_forward(p, dtype, (hipStream_t)stream);
   });
 }
@@ -98,7 +98,7 @@ int rabitq_grouped_matmul_dx(const rabitq_lists* l, int32_t dtype, const void* d
     if (!aligned(dout, sz) || !aligned(w, sz) || !aligned(dx, sz) || !aligned(scratch, 16)) return bad(call, "pointer not aligned to its type");
     hipStream_t st = (hipStream_t)stream;
     ProductArgs p = args_of(l);
-    p.a = dout; p.lda = ldd; p.b = w; p.ldb = ldw; p.stride = stride_w;
+    p.a = dout; p.lda = ldd; p.rows_a = l->pairs; p.b = w; p.ldb = ldw; p.stride = stride_w;
     if (l->nprobe == 1) {
       p.out = dx; p.ldo = ldx; p.out_dtype = dtype;
       return launch_product_dx(p, dtype, st);
@@ -136,7 +136,7 @@ int rabitq_grouped_matmul_dw(const rabitq_lists* l, int32_t dtype, const void* d
     const int64_t sz = dtype_bytes(dtype);
     if (!aligned(dout, sz) || !aligned(x, sz) || !aligned(dw, sz) || !aligned(scratch, 16)) return bad(call, "pointer not aligned to its type");
     ProductArgs p = args_of(l);
-    p.a = dout; p.lda = ldd; p.b = x; p.ldb = ldx; p.out = dw; p.ldo = ldw; p.stride = stride_w; p.out_dtype = dtype;
+    p.a = dout; p.lda = ldd; p.rows_a = l->pairs; p.b = x; p.ldb = ldx; p.out = dw; p.ldo = ldw; p.stride = stride_w; p.out_dtype = dtype;
     return launch_product_dw(p, dtype, static_cast<float*>(scratch), (hipStream_t)stream);
   });
 }
@@ -167,7 +167,7 @@ int rabitq_matmul_i8(const int8_t* a, int64_t lda, const float* scale_a, const i
     if (!a || !b || !scale_a || !scale_b || !out) return bad(call, "null pointer");
     if (!aligned(scale_a, 4) || !aligned(scale_b, 4) || !aligned(out, dtype_bytes(out_dtype))) return bad(call, "pointer not aligned to its type");
     ProductArgs p{};
-    p.a = a; p.lda = lda; p.b = b; p.ldb = ldb; p.scale_a = scale_a; p.scale_b = scale_b;
+    p.a = a; p.lda = lda; p.rows_a = m; p.b = b; p.ldb = ldb; p.scale_a = scale_a; p.scale_b = scale_b;
     p.pairs = m; p.n = n; p.k = k; p.groups = 1; p.probe = divisor(1); p.out = out; p.ldo = ldo; p.out_dtype = out_dtype;
     return launch_product_forward(p, DTYPE_I8, (hipStream_t)stream);
   });
@@ -187,7 +187,7 @@ int rabitq_grouped_matmul_i8(const rabitq_lists* l, const int8_t* x, int64_t ldx
     if (!x || !w || !scale_x || !scale_w || !out) return bad(call, "null pointer");
     if (!aligned(scale_x, 4) || !aligned(scale_w, 4) || !aligned(out, dtype_bytes(out_dtype))) return bad(call, "pointer not aligned to its type");
     ProductArgs p = args_of(l);
-    p.a = x; p.lda = ldx; p.b = w; p.ldb = ldw; p.stride = stride_w; p.scale_a = scale_x; p.scale_b = scale_w;
+    p.a = x; p.lda = ldx; p.rows_a = l->pairs / l->nprobe; p.b = w; p.ldb = ldw; p.stride = stride_w; p.scale_a = scale_x; p.scale_b = scale_w;
     p.out = out; p.ldo = ldo; p.out_dtype = out_dtype;
     return launch_product_forward(p, DTYPE_I8, (hipStream_t)stream);
   });

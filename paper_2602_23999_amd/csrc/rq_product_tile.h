@@ -64,6 +64,10 @@ __device__ __forceinline__ int j_of_row(int m) { return 16 * ((m >> 2) & 1) + 4 
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
+// The same from base + offset of the lane, base in scalar registers: nothing to compute per lane and step.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+}
 // (As builtins and not in the asm, so that the compiler's own count of LDS reads in flight starts again from none.)
 __device__ __forceinline__ void wait_and_barrier() {
   asm volatile("" ::: "memory");
@@ -104,8 +108,8 @@ __device__ __forceinline__ i32x4 load_piece(const char* from, int valid) {
 
 static __device__ __align__(16) unsigned char product_zeros[16];
 
-// FAST: every row of both operands starts at a multiple of 16 bytes and is whole pieces of 16 bytes long; pieces go to LDS without
-// registers.  Otherwise they are loaded element by element where a row ends inside one, and pass through registers.
+// FAST: every row of both operands starts at a multiple of 16 bytes and is whole pieces of 16 bytes long, and they lie near enough to
+// each other for 32-bit offsets (fast_rows); pieces go to LDS without registers.  Otherwise they are loaded element by element where a row ends inside one, and pass through registers.
 template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
 __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs p) {
   constexpr int NT = 64 * WI * WJ, SZ = sizeof(T), EPC = 16 / SZ, STEP = 128 / SZ;
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   extern __shared__ __align__(16) char smem[];
   int* row_pair = reinterpret_cast<int*>(smem + 2 * STAGE);  // [BI] pair of every row, or -1
   float* row_scale = reinterpret_cast<float*>(row_pair + BI);  // [BI] codes only
-  int* block_pairs = row_pair;                               // dw: [2][512] pairs of the positions
+  int2* block_pairs = reinterpret_cast<int2*>(row_pair);     // dw: [2][512] pairs of the positions and their rows of x, or -1
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
 
@@ -180,10 +184,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   const char* a = static_cast<const char*>(p.a);
   const char* b = static_cast<const char*>(p.b) + (OP == GRAD_W ? 0 : (int64_t)g * p.stride * SZ);
   const char* zeros = reinterpret_cast<const char*>(product_zeros);
+  asm("" : "+s"(zeros));  // (kept in registers, not made anew at every use)
 
   const int jleft = (int)(width - j0 < BJ ? width - j0 : BJ);  // columns of the tile that exist
-  // this thread's pieces of a step: where they start, and which c (or, of turned operands, which i or j) they hold
-  const char* pa[NA];
+  // this thread's pieces of a step: where they start (FAST: from the first row of a, or of the tile of b, less than 2^32 bytes behind
+  // it), and which c (or, of turned operands, which i or j) they hold
+  const char* pa[FAST ? 1 : NA];
+  uint32_t oa[FAST && !TA ? NA : 1], ob[FAST && !TA ? NB : 1];
   const int line = tid >> 3;
   const uint32_t ca = ((tid & 7) ^ swizzle_i(line)) * EPC, cb = ((tid & 7) ^ swizzle_j(line)) * EPC;  // (the same for all q)
   constexpr int PA = BI * SZ / 16, PB = BJ * SZ / 16;     // pieces of a line of a turned operand
@@ -192,17 +199,32 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     for (int q = 0; q < NA; ++q) {
       const int pr = row_pair[line + q * (NT / 8)];
       const int64_t row = pr < 0 ? 0 : OP == FORWARD ? p.probe.of(pr) : pr;  // (a row that is not there reads row 0, unused)
-      pa[q] = a + (row * p.lda + ca) * SZ;
+      if constexpr (FAST) oa[q] = (uint32_t)((row * p.lda + ca) * SZ);
+      else pa[q] = a + (row * p.lda + ca) * SZ;
     }
   }
   const char* pb = nullptr;  // piece 0; the others lie whole lines behind it
-  if constexpr (!TB) pb = b + ((j0 + line) * p.ldb + cb) * SZ;
-  if constexpr (OP == GRAD_X) pb = b + (tid / PB * p.ldb + j0) * SZ;
+  if constexpr (!FAST && !TB) pb = b + ((j0 + line) * p.ldb + cb) * SZ;
+  if constexpr (!FAST && OP == GRAD_X) pb = b + (tid / PB * p.ldb + j0) * SZ;
+  if constexpr (FAST && !TA) {  // (rows and columns that are not there read the first ones, unused)
+#pragma unroll
+    for (int q = 0; q < NB; ++q) {
+      if constexpr (!TB) {
+        const int row = line + q * (NT / 8);
+        ob[q] = (uint32_t)(((row < jleft ? row : 0) * p.ldb + cb) * SZ);
+      } else {
+        const int c = (tid + q * NT) / PB, col = swizzle_turned<SZ, PB>(c, (tid + q * NT) % PB) * EPC;
+        ob[q] = (uint32_t)((c * p.ldb + (col < jleft ? col : 0)) * SZ);
+      }
+    }
+    b += (!TB ? j0 * p.ldb : j0) * SZ;
+  }
   // dw: the pairs of this thread's lines, a step ahead (the lines of both operands are the same).  They come from a ring of two
   // blocks of positions in LDS: loads of their own would have to arrive within a step, and all loads are waited for in order.
   constexpr int LP = TA ? NA : 1, BLOCK = 512, FILL = BLOCK / NT;
   static_assert(!TA || (BI == BJ && BLOCK % NT == 0));
-  int pairs_next[LP], block_next[FILL > 0 ? FILL : 1];
+  int2 pairs_next[LP];
+  int block_next[FILL > 0 ? FILL : 1];
   auto load_block = [&](uint32_t block) {
     if constexpr (TA) {
 #pragma unroll
@@ -215,7 +237,10 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   auto store_block = [&](uint32_t block) {
     if constexpr (TA) {
 #pragma unroll
-      for (int f = 0; f < FILL; ++f) block_pairs[block % 2 * BLOCK + f * NT + tid] = block_next[f];
+      for (int f = 0; f < FILL; ++f) {
+        const int pr = block_next[f];
+        block_pairs[block % 2 * BLOCK + f * NT + tid] = int2{pr, pr < 0 ? -1 : p.probe.of(pr)};
+      }
     }
   };
   auto find_pairs = [&](uint32_t c0) {
@@ -224,15 +249,44 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       for (int q = 0; q < NA; ++q) pairs_next[q] = block_pairs[(c0 + (uint32_t)(tid + q * NT) / PA) % (2 * BLOCK)];
     }
   };
-  // where piece q of the step at c0 lies, and how many of its elements exist (none or more than there are, as may be)
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * 1024);
+  // FAST: the columns that a thread has of both operands of dw are the same in all its lines (none: a row of zeros)
+  const char *ga = zeros, *gb = zeros;
+  uint32_t ga_ld = 0, gb_ld = 0;
+  if constexpr (FAST && TA) {
+    const int col_a = swizzle_turned<SZ, PA>(tid / PA, tid % PA) * EPC, col_b = swizzle_turned<SZ, PB>(tid / PB, tid % PB) * EPC;
+    if (col_a < iend - i0) ga = a + (i0 + col_a) * SZ, ga_ld = (uint32_t)(p.lda * SZ);
+    if (col_b < jleft) gb = b + (j0 + col_b) * SZ, gb_ld = (uint32_t)(p.ldb * SZ);
+  }
+  // FAST: piece q of the step at c0, straight to LDS
+  auto fetch_piece = [&](int q, uint32_t c0, int buf) {
+    const uint32_t at = lds + buf * STAGE + (q < NA ? q * (NT * 16) : BI * 128 + (q - NA) * (NT * 16));
+    const int qa = q < NA ? q : 0, qb = q < NA ? 0 : q - NA;
+    if (c0 >= nc) return;
+    if constexpr (TA) {
+      const int row = q < NA ? pairs_next[qa].x : pairs_next[qb].y;
+      const char* from = (q < NA ? ga : gb) + (uint64_t)(uint32_t)row * (q < NA ? ga_ld : gb_ld);
+      load_to_lds(row < 0 ? zeros : from, at);
+    } else {
+      const char* base = q < NA ? a + (uint64_t)c0 * SZ : b + (TB ? (int64_t)c0 * p.ldb : (int64_t)c0) * SZ;
+      const uint32_t offset = q < NA ? oa[qa] : ob[qb];
+      if (c0 + STEP <= nc) {
+        load_to_lds(base, offset, at);
+      } else {  // the last step: zeros behind the end
+        const uint32_t c = c0 + (q < NA ? ca : !TB ? cb : (uint32_t)(tid + qb * NT) / PB);
+        load_to_lds(c < nc ? base + offset : zeros, at);
+      }
+    }
+  };
+  // else: where it lies, and how many of its elements exist (none or more than there are, as may be)
   auto piece_a = [&](int q, uint32_t c0, const char*& from) -> int {
     if constexpr (!TA) {
       from = pa[q] + (uint64_t)c0 * SZ;
       return c0 + ca < nc ? (int)(nc - c0 - ca) : 0;
     } else {
       const int col = swizzle_turned<SZ, PA>((tid + q * NT) / PA, (tid + q * NT) % PA) * EPC;
-      from = a + ((int64_t)pairs_next[q] * p.lda + i0 + col) * SZ;
-      return pairs_next[q] < 0 ? 0 : (int)(iend - i0) - col;
+      from = a + ((int64_t)pairs_next[q].x * p.lda + i0 + col) * SZ;
+      return pairs_next[q].x < 0 ? 0 : (int)(iend - i0) - col;
     }
   };
   auto piece_b = [&](int q, uint32_t c0, const char*& from) -> int {
@@ -245,16 +299,9 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       return c0 + c < nc ? jleft - piece * EPC : 0;
     } else {
       const int col = swizzle_turned<SZ, PB>((tid + q * NT) / PB, (tid + q * NT) % PB) * EPC;
-      from = b + ((int64_t)p.probe.of(pairs_next[q]) * p.ldb + j0 + col) * SZ;
-      return pairs_next[q] < 0 ? 0 : jleft - col;
+      from = b + ((int64_t)pairs_next[q].y * p.ldb + j0 + col) * SZ;
+      return pairs_next[q].y < 0 ? 0 : jleft - col;
     }
-  };
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  auto fetch_piece = [&](int q, uint32_t c0, int buf) {  // straight to LDS
-    const uint32_t at = lds + buf * STAGE + wave * 1024 + (q < NA ? q * (NT * 16) : BI * 128 + (q - NA) * (NT * 16));
-    const char* from;
-    const int valid = q < NA ? piece_a(q < NA ? q : 0, c0, from) : piece_b(q < NA ? 0 : q - NA, c0, from);
-    load_to_lds(valid > 0 ? from : zeros, at);
   };
   constexpr int RA = FAST ? 1 : NA, RB = FAST ? 1 : NB;
   i32x4 va[RA], vb[RB];
@@ -354,7 +401,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       if constexpr (HALF >= 0) {
 #pragma unroll
         for (int q = 0; q < NA + NB; ++q)
-          if (q * (2 * FI) / (NA + NB) == HALF * FI + x && (BI >= 256 || c2 < nc)) fetch_piece(q, c2, buf2);
+          if (q * (2 * FI) / (NA + NB) == HALF * FI + x) fetch_piece(q, c2, buf2);
       }
       __builtin_amdgcn_sched_barrier(0);
     }

@@ -27,6 +27,7 @@ struct ProductArgs {
   const void* b;
   void* out;
   int64_t lda, ldb, ldo;
+  int64_t rows_a;
   int64_t stride;             // between the matrices of two lists, in b or (dw) in out
   const float* scale_a;       // codes only: one per row of a, one per row of b ([groups][n])
   const float* scale_b;
