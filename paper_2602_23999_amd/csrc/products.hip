@@ -30,40 +30,53 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(ProductArgs p, T* __rest
         }
       }
       int64_t row = e0 / p.k, col = e0 % p.k;
-      for (int e = 0; e < here; ++e) {
-        out[(int64_t)g * p.stride + row * p.ldo + col] = (T)sum[e];
-        if (++col == p.k) { col = 0; ++row; }
+      T* to = out + (int64_t)g * p.stride + row * p.ldo + col;
+      if (col + 4 <= p.k) {
+        const T v[4] = {(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
+        __builtin_memcpy(to, v, sizeof(v));  // (at any alignment of the element)
+      } else {
+        for (int e = 0; e < here; ++e) {
+          out[(int64_t)g * p.stride + row * p.ldo + col] = (T)sum[e];
+          if (++col == p.k) { col = 0; ++row; }
+        }
       }
     }
   }
 }
 
-// dx of several probes: the named pairs' rows in ascending order of the pair.  A thread takes VEC neighbouring columns (4 where k
-// and the output allow it) of a query.
-template <class T, int VEC>
+// dx of several probes: the named pairs' rows in ascending order of the pair.  A thread takes 4 neighbouring columns of a query.
+template <class T>
 __global__ __launch_bounds__(256) void sum_named_kernel(const float* __restrict__ parts, const uint8_t* __restrict__ named, int64_t rows,
                                                         int nprobe, int k, T* __restrict__ out, int64_t ldo) {
-  const int per_row = k / VEC;
+  const int per_row = (k + 3) / 4;
   const int64_t all = rows * per_row;
   for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
     const int64_t q = id / per_row;
-    const int j = (int)(id - q * per_row) * VEC;
-    float sum[VEC] = {};
+    const int j = (int)(id - q * per_row) * 4, here = min(4, k - j);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
     bool any = false;
     for (int r = 0; r < nprobe; ++r) {
       const int64_t pr = q * nprobe + r;
       if (!named[pr]) continue;
       any = true;
-      float v[VEC];
-      __builtin_memcpy(v, parts + pr * k + j, 4 * VEC);
+      const float* from = parts + pr * k + j;
+      if (here == 4) {
+        float v[4];
+        __builtin_memcpy(v, from, 16);  // (at any alignment of the element, as below)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[e] += v[e];
+        for (int e = 0; e < 4; ++e) sum[e] += v[e];
+      } else {
+        for (int e = 0; e < here; ++e) sum[e] += from[e];
+      }
     }
     if (!any) continue;
-    T o[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) o[e] = (T)sum[e];
-    __builtin_memcpy(out + q * ldo + j, o, sizeof(T) * VEC);
+    T* to = out + q * ldo + j;
+    if (here == 4) {
+      const T v[4] = {(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
+      __builtin_memcpy(to, v, sizeof(v));
+    } else {
+      for (int e = 0; e < here; ++e) to[e] = (T)sum[e];
+    }
   }
 }
 
@@ -208,10 +221,8 @@ int launch_clear_bytes(void* at, int64_t n, hipStream_t st) {
 
 template <class T>
 static int sum_named(const float* parts, const uint8_t* named, int64_t rows, int nprobe, int k, T* out, int64_t ldo, hipStream_t st) {
-  const bool four = k % 4 == 0 && ldo % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
-  const unsigned grid = (unsigned)std::min<int64_t>(up(rows * (k / (four ? 4 : 1)), 256), 1 << 20);
-  if (four) sum_named_kernel<T, 4><<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, out, ldo);
-  else sum_named_kernel<T, 1><<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, out, ldo);
+  const unsigned grid = (unsigned)std::min<int64_t>(up(rows * up(k, 4), 256), 1 << 20);
+  sum_named_kernel<T><<<grid, 256, 0, st>>>(parts, named, rows, nprobe, k, out, ldo);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }

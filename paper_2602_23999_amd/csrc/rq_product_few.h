@@ -99,12 +99,18 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p) {
     for (int e = 0; e < 4; ++e) v[e] = v[e] * sa * sb[j + e < p.n ? j + e : 0];
   }
   const int64_t at = pair * p.ldo + j;
-  if (j + 4 <= p.n && (p.ldo & 3) == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0) {
+  if (j + 4 <= p.n) {  // (at any alignment of the element)
     typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    if (p.out_dtype == RABITQ_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = v;
-    else if (p.out_dtype == RABITQ_F16) *reinterpret_cast<f16x4*>(static_cast<_Float16*>(p.out) + at) = __builtin_convertvector(v, f16x4);
-    else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + at) = __builtin_convertvector(v, bf16x4);
+    if (p.out_dtype == RABITQ_F32) {
+      __builtin_memcpy(static_cast<float*>(p.out) + at, &v, 16);
+    } else if (p.out_dtype == RABITQ_F16) {
+      const f16x4 h = __builtin_convertvector(v, f16x4);
+      __builtin_memcpy(static_cast<_Float16*>(p.out) + at, &h, 8);
+    } else {
+      const bf16x4 h = __builtin_convertvector(v, bf16x4);
+      __builtin_memcpy(static_cast<__bf16*>(p.out) + at, &h, 8);
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)

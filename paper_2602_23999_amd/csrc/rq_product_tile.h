@@ -466,7 +466,6 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   constexpr int COLS = FJ * 32, PIECES = COLS / 4;  // of a row: a power of two
   static_assert(32 * COLS * 4 * WI * WJ <= 2 * STAGE && (PIECES & (PIECES - 1)) == 0 && PIECES >= 8);
   const int each = out_dtype == RABITQ_F32 ? 4 : 8;  // columns that a lane stores at once
-  const bool whole = (ldo | ostride) % each == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
   f32x4* mine = reinterpret_cast<f32x4*>(smem) + wave * (32 * PIECES);
   const int per_row = COLS / each, rows_at_once = 64 / per_row;
   const int col = lane % per_row * each;
@@ -507,10 +506,16 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
           hi[e] = hi[e] * sa * sb[4 + e];
         }
       }
-      if (whole && j + each <= width) {
-        if (out_dtype == RABITQ_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = lo;
-        else if (out_dtype == RABITQ_F16) *reinterpret_cast<f16x8*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), f16x8);
-        else *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+      if (j + each <= width) {  // (at any alignment of the element)
+        if (out_dtype == RABITQ_F32) {
+          __builtin_memcpy(static_cast<float*>(out) + at, &lo, 16);
+        } else if (out_dtype == RABITQ_F16) {
+          const f16x8 v = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), f16x8);
+          __builtin_memcpy(static_cast<_Float16*>(out) + at, &v, 16);
+        } else {
+          const bf16x8 v = __builtin_convertvector(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+          __builtin_memcpy(static_cast<__bf16*>(out) + at, &v, 16);
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
