@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void sum_named_kernel(const float* __restrict_
 
 static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
-template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
+template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, bool FAST>
 static int launch_tiles(ProductArgs p, hipStream_t st) {
   const int64_t width = OP == FORWARD ? p.n : p.k;
   p.tiles_i = OP == GRAD_W ? up(p.n, BI) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups)
@@ -93,19 +93,19 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
   p.strips = (uint32_t)strips;
   p.strip = (uint32_t)strip;
   const int64_t grid = up(p.tiles_i * strips, 8) * 8 * strip;
-  if (grid > MAX_GRID / (64 * WI * WJ)) {
+  if (grid > MAX_GRID / (64 * WI * WJ * KS)) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
-  const size_t lds = 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int2) : BI * (sizeof(int) + sizeof(float)));
-  auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, FAST>;
+  const size_t lds = KS * 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int2) : BI * (sizeof(int) + sizeof(float)));
+  auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, KS, FAST>;
   if (p.check_only) return RABITQ_OK;
   static bool granted = false;  // more LDS than a launch gets unasked
   if (!granted) {
     RQ_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     granted = true;
   }
-  kernel<<<(unsigned)grid, 64 * WI * WJ, lds, st>>>(p);
+  kernel<<<(unsigned)grid, 64 * WI * WJ * KS, lds, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }
@@ -160,19 +160,30 @@ static int tile_size(const ProductArgs& p, int op, int size) {
   return 64;
 }
 
+// Whether four groups of wavefronts share a 64 x 64 tile of a forward or dx product: with little more than a tile for each compute unit,
+// and 8 steps of contraction or more (256 x 4096 x 4096 codes, 256 tiles: 22 us, shared 14; 326 rows, 2 lists, 1222 x 7352 fp16:
+// 73 and 47; 2000 rows, 4 lists, 512 x 1024 bf16, 280 tiles: 13.6 and 14.2; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 20 and 28).
+static bool share_tiles(const ProductArgs& p, int op, int size) {
+  const int64_t width = op == FORWARD ? p.n : p.k, contraction = op == FORWARD ? p.k : p.n;
+  const int64_t rows = std::min<int64_t>(p.pairs, p.pair_off ? p.pairs / 64 + p.groups : up(p.pairs, 64));
+  return contraction * size >= 8 * 128 && rows * up(width, 64) <= 280;
+}
+
 template <class T, int OP>
 static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
     if (few_rows(p)) return launch_few<T>(p, st);
   }
   const int edge = tile_size(p, OP, sizeof(T));
-  if (!fast_rows(p, OP, dtype))
-    return edge > 64 ? launch_tiles<T, OP, 128, 128, 2, 2, false>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, false>(p, st);
-  switch (edge) {
-    case 256: return launch_tiles<T, OP, 256, 256, 2, 4, true>(p, st);
-    case 128: return launch_tiles<T, OP, 128, 128, 2, 2, true>(p, st);
+  const bool fast = fast_rows(p, OP, dtype);
+  if (edge == 256 && fast) return launch_tiles<T, OP, 256, 256, 2, 4, 1, true>(p, st);
+  if (edge > 64)
+    return fast ? launch_tiles<T, OP, 128, 128, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 128, 128, 2, 2, 1, false>(p, st);
+  if constexpr (OP != GRAD_W) {
+    if (share_tiles(p, OP, sizeof(T)))
+      return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 4, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 4, false>(p, st);
   }
-  return launch_tiles<T, OP, 64, 64, 2, 2, true>(p, st);
+  return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 1, false>(p, st);
 }
 
 template <int OP>

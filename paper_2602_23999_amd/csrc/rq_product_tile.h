@@ -110,19 +110,25 @@ static __device__ __align__(16) unsigned char product_zeros[16];
 
 // FAST: every row of both operands starts at a multiple of 16 bytes and is whole pieces of 16 bytes long, and they lie near enough to
 // each other for 32-bit offsets (fast_rows); pieces go to LDS without registers.  Otherwise they are loaded element by element where a row ends inside one, and pass through registers.
-template <class T, int OP, int BI, int BJ, int WI, int WJ, bool FAST>
-__global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs p) {
+//
+// KS: groups of wavefronts that share a tile, each with its own part of the contraction and its own steps in LDS; their sums are added
+// up in order at the end.  For long contractions of so few tiles that most of the chip would be idle.
+template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, bool FAST>
+__global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(ProductArgs p) {
   constexpr int NT = 64 * WI * WJ, SZ = sizeof(T), EPC = 16 / SZ, STEP = 128 / SZ;
   constexpr bool TA = OP == GRAD_W, TB = OP != FORWARD;
   constexpr int NA = BI * 8 / NT, NB = BJ * 8 / NT;       // pieces per thread and step
   constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;     // 32 x 32 products per wavefront
   constexpr int STAGE = (BI + BJ) * 128;
   using Acc = typename Mma<T>::Acc;
-  extern __shared__ __align__(16) char smem[];
-  int* row_pair = reinterpret_cast<int*>(smem + 2 * STAGE);  // [BI] pair of every row, or -1
+  static_assert(KS == 1 || !TA);
+  extern __shared__ __align__(16) char smem_all[];
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ks = wave_all / (WI * WJ);
+  char* smem = smem_all + ks * (2 * STAGE);
+  int* row_pair = reinterpret_cast<int*>(smem_all + KS * 2 * STAGE);  // [BI] pair of every row, or -1
   float* row_scale = reinterpret_cast<float*>(row_pair + BI);  // [BI] codes only
   int2* block_pairs = reinterpret_cast<int2*>(row_pair);     // dw: [2][512] pairs of the positions and their rows of x, or -1
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x % NT, lane = tid & 63, wave = wave_all % (WI * WJ);  // of the group
   const int wi = wave / WJ, wj = wave % WJ;
 
   // which tile
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     iend = s.end;
     if (i0 < s.begin || i0 >= iend) return;
     nc = OP == FORWARD ? p.k : (uint32_t)p.n;
-    for (int i = tid; i < BI; i += NT) {
+    for (int i = threadIdx.x; i < BI; i += NT * KS) {
       const int pr = i0 + i < iend ? (int)pair_at(p, i0 + i) : -1;
       row_pair[i] = pr;
       if constexpr (SZ == 1) row_scale[i] = pr < 0 ? 0.f : p.scale_a[p.probe.of(pr)];
@@ -183,6 +189,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   }
   const char* a = static_cast<const char*>(p.a);
   const char* b = static_cast<const char*>(p.b) + (OP == GRAD_W ? 0 : (int64_t)g * p.stride * SZ);
+  uint32_t span = nc;  // that a group goes over, in whole steps where there are several
+  if constexpr (KS > 1) {
+    span = ((nc + STEP - 1) / STEP + KS - 1) / KS * STEP;
+    const uint32_t begin = ks * span;
+    nc = begin < nc ? min(nc - begin, span) : 0;
+    a += (uint64_t)begin * SZ;
+    b += (TB ? (int64_t)begin * p.ldb : (int64_t)begin) * SZ;
+  }
   const char* zeros = reinterpret_cast<const char*>(product_zeros);
   asm("" : "+s"(zeros));  // (kept in registers, not made anew at every use)
 
@@ -262,7 +276,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
   auto fetch_piece = [&](int q, uint32_t c0, int buf) {
     const uint32_t at = lds + buf * STAGE + (q < NA ? q * (NT * 16) : BI * 128 + (q - NA) * (NT * 16));
     const int qa = q < NA ? q : 0, qb = q < NA ? 0 : q - NA;
-    if (c0 >= nc) return;
+    if (c0 >= span) return;
     if constexpr (TA) {
       const int row = q < NA ? pairs_next[qa].x : pairs_next[qb].y;
       const char* from = (q < NA ? ga : gb) + (uint64_t)(uint32_t)row * (q < NA ? ga_ld : gb_ld);
@@ -421,7 +435,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       fetch_regs(c0);
     }
   };
-  if (nc > 0) {
+  if (span > 0) {
     if constexpr (TA) {
       load_block(0);
       store_block(0);
@@ -444,7 +458,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
       fetch_regs(STEP);
     }
     int buf = 0;
-    for (uint32_t c0 = 0; c0 < nc; c0 += STEP, buf ^= 1) {
+    for (uint32_t c0 = 0; c0 < span; c0 += STEP, buf ^= 1) {
       // (the first step of block b: nobody looks at block b - 1 any more, and b + 1 is there)
       const bool refill = TA && c0 != 0 && c0 % BLOCK == 0;
       multiply(sub0, buf, second, c0 + STEP, buf ^ 1);
@@ -461,6 +475,27 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
     __builtin_amdgcn_s_waitcnt(0x0070);  // nothing may be on its way to LDS when the workgroup ends
   }
 
+  if constexpr (KS > 1) {
+    static_assert(FI * FJ * 64 * NT <= 2 * STAGE);
+    Acc* sums = reinterpret_cast<Acc*>(smem_all);  // [group][product][thread]
+    constexpr int PER_GROUP = 2 * STAGE / (int)sizeof(Acc);
+    __syncthreads();  // (the last operands have been read)
+    if (ks > 0) {
+#pragma unroll
+      for (int x = 0; x < FI; ++x)
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) sums[ks * PER_GROUP + (x * FJ + y) * NT + tid] = acc[x][y];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int u = 1; u < KS; ++u)
+#pragma unroll
+      for (int x = 0; x < FI; ++x)
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) acc[x][y] += sums[u * PER_GROUP + (x * FJ + y) * NT + tid];
+  }
+
   // A lane has 16 neighbouring columns of a row, so a store of its own would touch 32 rows for 16 bytes each.  The wavefront's 32
   // rows go through LDS instead (its own part of it, as fp32, pieces of 16 bytes swizzled by the row) and out in whole rows of COLS.
   constexpr int COLS = FJ * 32, PIECES = COLS / 4;  // of a row: a power of two
@@ -475,7 +510,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_tile_kernel(ProductArgs 
 #pragma unroll
     for (int e = 0; e < 8; ++e) sb[e] = e < each && j + e < width ? p.scale_b[(int64_t)g * p.n + j + e] : 0.f;
   }
-  __syncthreads();  // (the last operands have been read)
+  if constexpr (KS == 1) __syncthreads();  // (the last operands have been read)
 #pragma unroll
   for (int x = 0; x < FI; ++x) {
 #pragma unroll

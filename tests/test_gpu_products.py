@@ -212,6 +212,35 @@ def test_large_products(rows, groups, odd, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("nq,nprobe,groups,wide,long", [
+    (300, 2, 3, 130, 1100),
+    (301, 1, 3, 129, 1111),     # rows that do not start at multiples of 16 bytes
+    (200, 1, 1, 64, 520),       # of four parts of the contraction the last is empty (16-bit types)
+    (200, 1, 1, 64, 263),       # ... (f32), and one ends inside a step
+    (700, 1, 2, 72, 8200),
+], ids=str)
+def test_few_tiles_of_a_long_contraction(nq, nprobe, groups, wide, long, dtype):
+    off, ids = lists_from(probes_of(nq, nq, nprobe, groups, 0, 0.05), groups)
+    lists = off.cuda(), ids.cuda(), nprobe
+    x, w = numbers(1, (nq, long), dtype), numbers(2, (groups, wide, long), dtype)
+    want, mag, named = forward64(x, w, off, ids, nprobe)
+    got = rabitq.grouped_matmul(x.cuda(), w.cuda(), *lists, out=torch.full((nq * nprobe, wide), 7.0, dtype=dtype, device="cuda"))
+    assert_sums(got[named], want[named], mag[named], long, dtype)
+    assert (got[~named] == 7.0).all()
+    dy, w = numbers(3, (nq * nprobe, long), dtype), numbers(4, (groups, long, wide), dtype)
+    want, mag, named = dx64(dy, w, off, ids, nprobe)
+    got = rabitq.grouped_matmul_dx(dy.cuda(), w.cuda(), *lists, out=torch.full((nq, wide), 7.0, dtype=dtype, device="cuda"))
+    assert_sums(got[named], want[named], mag[named], long * nprobe, dtype)
+    assert (got[~named] == 7.0).all()
+    if dtype == torch.float32:
+        (cx, sx), (cw, sw) = codes64(x), codes64(numbers(2, (groups * wide, long), dtype))
+        cw, sw = cw.reshape(groups, wide, long), sw.reshape(groups, wide)
+        want, named = grouped_i8_64(cx, sx, cw, sw, off, ids, nprobe)
+        got = rabitq.grouped_matmul_i8(cx.cuda(), sx.cuda(), cw.cuda(), sw.cuda(), *lists)
+        assert_scaled(got[named], want[named], dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("nq,nprobe,groups,n,k", [
     (500, 2, 4, 2048, 2056),    # 256 x 256 tiles
     (900, 1, 8, 1000, 1032),    # 128 x 128 tiles
@@ -233,7 +262,8 @@ def test_large_dw(nq, nprobe, groups, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
-@pytest.mark.parametrize("m,n,k", [(4200, 4100, 528), (1100, 8200, 272), (1030, 8195, 515), (48, 5000, 3000), (40, 70000, 100)])
+@pytest.mark.parametrize("m,n,k", [(4200, 4100, 528), (1100, 8200, 272), (1030, 8195, 515), (48, 5000, 3000), (40, 70000, 100), (300, 200, 4100),
+                                   (290, 190, 4111)])
 def test_large_matmul_i8(m, n, k, dtype):
     g = torch.Generator().manual_seed(m)
     a, b = (torch.randint(-128, 128, (r, k), generator=g).to(torch.int8).cuda() for r in (m, n))
