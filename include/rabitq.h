@@ -342,17 +342,18 @@ int rabitq_merge(rabitq_index_t index, const uint64_t* cand_keys, const int32_t*
  * may be captured into a HIP graph.  Two calls may overlap in time if neither writes what the other reads or writes.
  * Matrices are row-major with a row stride ("ld...", in elements, at least the row's length); any stride and any alignment of
  * the element type is taken, rows that start at multiples of 16 bytes are the fast case.  Outputs must not overlap inputs.
- * Sums are fp32 (int32 for codes) and are taken in an order that depends on the sizes only: equal calls give equal bits. */
+ * Sums are fp32 (int32 for codes) and are taken in an order that depends on sizes, types and alignment only: equal calls give equal bits. */
 typedef enum { RABITQ_F32 = 0, RABITQ_F16 = 1, RABITQ_BF16 = 2 } rabitq_dtype;
 
 /* The pairs of a batch, regrouped by list.  List g holds the positions pair_off[g] .. pair_off[g+1) and its matrix W[g]
  * is [n][k]; position i stands for pair p = pair_ids[i], which belongs to row p / nprobe of the inputs x.  pair_off and pair_ids
  * are those of rabitq_build_probe_lists; rows that were sorted by list beforehand need no pair_ids (position i is pair i).
- * Offsets are taken as if they lay in [0, pairs], and a position whose pair id lies outside [0, pairs) is passed over.  A pair may be
- * named once: of a pair named more often, one of the results is written (and its gradient is one of the
- * terms).  Positions outside every list take part in nothing. */
+ * Offsets must ascend (equal ones are an empty list); they are taken as if they lay in [0, pairs], and a position whose pair id lies
+ * outside [0, pairs) is passed over.  Offsets that descend give results that say nothing, within the outputs.  A pair should be
+ * named once: of a pair named more often, each element of its row is that of one of the results, and any (and the gradient
+ * of x counts it once).  Positions outside every list take part in nothing. */
 typedef struct {
-  int32_t groups;          /* lists, >= 1                                              */
+  int32_t groups;          /* lists, 1 .. 2^24                                         */
   int32_t nprobe;          /* pairs per row of x, >= 1                                 */
   int64_t pairs;           /* rows of x times nprobe, 0 .. 2^31 - 1                    */
   int32_t n, k;            /* rows and columns of each list's matrix, 1 .. 2^20        */
@@ -363,8 +364,8 @@ typedef struct {
 /* out[p] = W[list of p] x[p / nprobe] for every pair named: out [pairs][n], x [pairs / nprobe][k], W [groups][n][k] with
  * stride_w elements from one matrix to the next (at least (n - 1) ldw + k), all of type `dtype`; one rounding, of the fp32 sum.
  * Rows of pairs that no list names are left as they were.
- * Errors (all calls of this section): RABITQ_EINVAL (null pointer, size or stride out of range, unknown type, more than
- * 2^23 tiles of work), RABITQ_EHIP. */
+ * Errors (all calls of this section): RABITQ_EINVAL (null pointer, size or stride out of range, unknown type, more tiles of
+ * work than one launch takes: 2^32 threads), RABITQ_EHIP. */
 int rabitq_grouped_matmul(const rabitq_lists* lists, int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw,
                           int64_t stride_w, void* out, int64_t ldo, void* stream);
 

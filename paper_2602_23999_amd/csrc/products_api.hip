@@ -9,6 +9,7 @@ namespace {
 
 constexpr int64_t MAX_WIDTH = 1 << 20;
 constexpr int64_t MAX_K_I8 = 131071;       // 128 x 128 x k must stay below 2^31
+constexpr int32_t MAX_LISTS = 1 << 24;
 constexpr int64_t MAX_LD = (int64_t)1 << 40;
 
 int bad(const char* call, const char* what) {
@@ -35,7 +36,7 @@ bool stride_ok(const rabitq_lists* l, int64_t ldw, int64_t stride) {
 
 int check_lists(const char* call, const rabitq_lists* l) {
   if (!l) return bad(call, "null pointer");
-  if (l->groups < 1) return bad(call, "groups must be at least 1");
+  if (l->groups < 1 || l->groups > MAX_LISTS) return bad(call, "groups must lie in 1 .. 2^24");
   if (l->nprobe < 1) return bad(call, "nprobe must be at least 1");
   if (l->pairs < 0 || l->pairs > 0x7fffffff) return bad(call, "pairs must lie in 0 .. 2^31 - 1");
   if (l->pairs % l->nprobe != 0) return bad(call, "pairs must be a multiple of nprobe");

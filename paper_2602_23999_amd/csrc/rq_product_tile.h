@@ -109,7 +109,8 @@ __device__ __forceinline__ i32x4 load_piece(const char* from, int valid) {
 static __device__ __align__(16) unsigned char product_zeros[16];
 
 // FAST: every row of both operands starts at a multiple of 16 bytes and is whole pieces of 16 bytes long, and they lie near enough to
-// each other for 32-bit offsets (fast_rows); pieces go to LDS without registers.  Otherwise they are loaded element by element where a row ends inside one, and pass through registers.
+// each other for 32-bit offsets (fast_rows); pieces go to LDS without registers.  Otherwise they are loaded element by element where a
+// row ends inside one, and pass through registers.
 //
 // KS: groups of wavefronts that share a tile, each with its own part of the contraction and its own steps in LDS; their sums are added
 // up in order at the end.  For long contractions of so few tiles that most of the chip would be idle.
@@ -391,8 +392,8 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
   // A step is multiplied in four parts of 32 bytes of every line; the operands of the next part are read while one is multiplied.
   // The one barrier of a step stands in front of its last part, where everybody has read the whole step and the next one, requested
   // a step ago, has arrived; behind it the step after that is requested into the half that is free, one half of its pieces during
-  // that part and the other during the next.  Reads and requests are dealt out among the products.  Behind the last step all this goes on for nothing (old lines of LDS, pieces of zeros), which is cheaper than
-  // a branch around each.
+  // that part and the other during the next.  Reads and requests are dealt out among the products.  Behind the last step the reads go
+  // on for nothing (old lines of LDS).
   i32x4 ai[2][FI], bj[2][FJ];
   auto read_one = [&](const char* st, int r, int sub, int set) {
     if (r < FJ) bj[set][r < FJ ? r : 0] = frag_j(st, r < FJ ? r : 0, sub);
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
     for (int r = 0; r < FI + FJ; ++r) read_one(smem, r, 0, 0);
     if constexpr (FAST) {
 #pragma unroll
-      for (int q = 0; q < NA + NB; ++q) 
+      for (int q = 0; q < NA + NB; ++q)
         if (q * (2 * FI) / (NA + NB) < FI) fetch_piece(q, STEP, 1);
     } else {
       fetch_regs(STEP);

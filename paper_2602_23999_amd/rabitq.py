@@ -428,8 +428,16 @@ def _vector(t, dtype, shape, what: str, dev: int) -> int:
     return ptr
 
 
+def _int32(n: int, what: str) -> int:
+    """n, which a 32-bit argument carries (ctypes would cut it off without a word)."""
+    if n > 0x7fffffff:
+        raise RabitqError(f"{n} {what} are too many")
+    return n
+
+
 def _lists_of(groups: int, n: int, k: int, pairs: int, nprobe: int, pair_off, pair_ids, dev: int) -> "_Lists":
-    return _Lists(groups, nprobe, pairs, n, k, _vector(pair_off, torch.int32, (groups + 1,), "pair_off", dev),
+    return _Lists(_int32(groups, "lists"), nprobe, pairs, _int32(n, "rows of a matrix"), _int32(k, "elements of a row"),
+                  _vector(pair_off, torch.int32, (groups + 1,), "pair_off", dev),
                   None if pair_ids is None else _vector(pair_ids, torch.int32, (pairs,), "pair_ids", dev))
 
 
@@ -508,7 +516,7 @@ def quantize_rows(x, codes=None, scale=None):
     codes, pc, ldc, _ = _output(codes, (rows, k), torch.int8, x, dev, "codes")
     if scale is None:
         scale = x.new_empty(rows, dtype=torch.float32)
-    _check(load_library().rabitq_quantize_rows(px, DTYPES[dt], ldx, rows, k, pc, ldc,
+    _check(load_library().rabitq_quantize_rows(px, DTYPES[dt], ldx, rows, _int32(k, "elements of a row"), pc, ldc,
                                                _vector(scale, torch.float32, (rows,), "scale", dev),
                                                torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale
@@ -525,7 +533,8 @@ def matmul_i8(a, scale_a, b, scale_b, out_dtype=torch.float32, out=None):
         raise RabitqError("out_dtype must be float32, float16 or bfloat16")
     out, po, ldo, _ = _output(out, (m, n), out_dtype, a, dev)
     _check(load_library().rabitq_matmul_i8(pa, lda, _vector(scale_a, torch.float32, (m,), "scale_a", dev), pb, ldb,
-                                           _vector(scale_b, torch.float32, (n,), "scale_b", dev), m, n, k, po,
+                                           _vector(scale_b, torch.float32, (n,), "scale_b", dev), m, n,
+                                           _int32(k, "elements of a row"), po,
                                            DTYPES[out_dtype], ldo, torch._C._cuda_getCurrentRawStream(dev)))
     return out
 

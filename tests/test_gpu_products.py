@@ -582,6 +582,17 @@ def test_binding_refusals():
         assert rabitq.grouped_matmul(x.requires_grad_(), w, off, ids, out=torch.zeros(6, 5, device="cuda")).abs().sum() == 0
 
 
+def test_rows_behind_32_bits_are_refused():
+    long = torch.empty(1, (1 << 32) + 16, dtype=torch.int8, device="cuda")  # (16 elements, were the length cut off)
+    s = torch.ones(1, device="cuda")
+    off = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for call in (lambda: rabitq.matmul_i8(long, s, long, s),
+                 lambda: rabitq.grouped_matmul_i8(long, s, long[None], s[None], off),
+                 lambda: rabitq.quantize_rows(long.view(torch.bfloat16).new_empty(1, (1 << 32) + 16))):
+        with pytest.raises(rabitq.RabitqError, match="too many"):
+            call()
+
+
 # ---- together -------------------------------------------------------------------------
 
 def test_a_layer_of_experts_behind_the_index():

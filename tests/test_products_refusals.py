@@ -72,6 +72,20 @@ def test_arguments_out_of_range(name, bad):
     assert rabitq.load_library().rabitq_last_error()
 
 
+@pytest.mark.parametrize("name", ["fwd", "dx", "dw", "gi8"])
+def test_number_of_lists_is_bounded(name):
+    assert _calls()[name](ls=_ls(groups=(1 << 24) + 1)) == -1
+    assert b"2^24" in rabitq.load_library().rabitq_last_error()
+
+
+def test_sizes_behind_32_bits_are_not_cut_off():
+    big = (1 << 32) + 16
+    off = torch.zeros(5, dtype=torch.int32)
+    for sizes in ((big, 8, 16), (4, big, 16), (4, 8, big)):
+        with pytest.raises(rabitq.RabitqError, match="too many"):
+            rabitq._lists_of(*sizes, 6, 2, off, None, 0)
+
+
 def test_k_of_codes_by_list_is_bounded():
     k = 131072
     assert _calls()["gi8"](ls=_ls(k=k), ldx=k, ldw=k, stride=8 * k) == -1
