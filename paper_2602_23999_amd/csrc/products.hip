@@ -100,11 +100,7 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
   const size_t lds = KS * 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int2) : BI * (sizeof(int) + sizeof(float)));
   auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, KS, FAST>;
   if (p.check_only) return RABITQ_OK;
-  static bool granted = false;  // more LDS than a launch gets unasked
-  if (!granted) {
-    RQ_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    granted = true;
-  }
+  if (lds > 64 * 1024) RQ_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
   kernel<<<(unsigned)grid, 64 * WI * WJ * KS, lds, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
@@ -121,15 +117,20 @@ static bool fast_rows(const ProductArgs& p, int op, int dtype) {
          rows_a * p.lda * sz < reach && 256 * p.ldb * sz < reach;
 }
 
-// Whether the forward product goes to the kernel that streams the matrices.  It reads them once per 16 rows, the tile kernel once per 128 or
-// 256; with at most 8 rows per list on average (16 of a single list, whose rows are known) that is once in both, and it needs no
-// LDS and no barriers (64 lists of 2048 x 2048 bf16, 4 rows each: 120 us and 152, 16 rows each: 187 and 182; one query against
-// 200 000 rows of 768 codes: 32 and 68).  Beyond, while the tile kernel would have less than 128 tiles of 128 columns to spread
-// over the chip, it still is the faster up to 48 rows (48 rows, 8192 x 8192 codes: 47 and 69; 32 rows, 50 000 x 768: 21 and 16).
-static bool few_rows(const ProductArgs& p) {
+// Whether the forward product goes to the kernel that streams the matrices, in 16 x 16 tiles and without LDS.  With at most 8 rows per
+// list on average (16 of a single list, whose rows are known) it reads every matrix once, as the tile kernel does, and waits for
+// nothing (64 lists of 2048 x 2048 bf16, 4 rows each: 120 us and 152, 16 rows each: 187 and 182; one query against 200 000 rows of 768
+// codes: 32 and 68).  Beyond, it reads more than the tile kernel, but has 16 times as many workgroups, which pays while those
+// are two for each compute unit that the tile kernel can fill (codes, 512 tiles of 16: 17 x 4096 x 4096 9.1 and 12.8 us, 128 x 512 x 8192
+// 11 and 20; 256 tiles, 1000 rows by 128 x 768: 3.9 and 6.1; more: 64 x 4096 x 4096 17 and 14, 48 x 8192 x 8192 46 and 26).
+// fp32 tiles are bound by the multiplication, of which this kernel wastes less: four for each (1024 tiles, 64 x 4096 x 1024:
+// 18 and 22; 768, 96 x 2048 x 16 384: 172 and 253).
+static bool few_rows(const ProductArgs& p, int size) {
   const int64_t lists = p.groups;
   if (p.pairs <= (p.pair_off ? 8 : 16) * lists) return true;
-  return p.pairs <= 48 * lists && std::min(lists, p.pairs) * up(p.n, 128) < 128;
+  const int64_t tiles16 = (p.pair_off ? p.pairs / 16 + lists : up(p.pairs, 16)) * up(p.n, 16);
+  const int64_t tiles64 = (p.pair_off ? p.pairs / 64 + lists : up(p.pairs, 64)) * up(p.n, 64);
+  return tiles16 <= (size == 4 ? 1024 : 512) * up(tiles64, 256);
 }
 
 template <class T>
@@ -172,7 +173,7 @@ static bool share_tiles(const ProductArgs& p, int op, int size) {
 template <class T, int OP>
 static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
-    if (few_rows(p)) return launch_few<T>(p, st);
+    if (few_rows(p, sizeof(T))) return launch_few<T>(p, st);
   }
   const int edge = tile_size(p, OP, sizeof(T));
   const bool fast = fast_rows(p, OP, dtype);
@@ -199,6 +200,7 @@ static int launch_op(const ProductArgs& p, int dtype, hipStream_t st) {
 
 int launch_product_forward(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<FORWARD>(p, dtype, st); }
 int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st) { return launch_op<GRAD_X>(p, dtype, st); }
+
 // Without parts a list occupies one workgroup per tile of its matrix, however long it is, so parts are for launches that would
 // leave places of the chip free: fewer than 512 tiles of 128 x 128 (two for each compute unit).  A part is as long as fills those places,
 // at least 512 positions, so that adding up costs less than it gains: 65 536 positions, 1 list, 512 x 512 bf16: 723 to 1449 us

@@ -1,8 +1,8 @@
-// The forward products with few rows per list: single tokens, one query against many stored rows.
+// The forward products with few rows per list (single tokens, one query against many stored rows) or few tiles at all.
 //
 // Every matrix is read once for a handful of rows, so the time is that of reading the matrices: they go straight from memory to the
 // registers in which the matrix instructions take them, many loads ahead, and nothing passes through LDS.  A tile is 16 positions of a
-// list.
+// list by 16 columns.
 #pragma once
 #include "rq_product_tile.h"
 

@@ -348,6 +348,34 @@ def test_strides_and_alignment_of_codes(m, n, k, pad, shift):
     assert _untouched(codes, flat)
 
 
+@pytest.mark.parametrize("dtype", [*TYPES, torch.int8], ids=str)
+@pytest.mark.parametrize("pad,shift", [(0, 0), (16, 16), (1, 0), (5, 3)])
+@pytest.mark.parametrize("nq,nprobe,groups,n,k", [
+    (1100, 2, 3, 1032, 272),
+    (1100, 2, 3, 1031, 77),
+    (600, 1, 2, 1000, 1120),  # few tiles of 64 x 64 of a long contraction, but many of 16 x 16
+    (600, 1, 2, 1001, 1111),
+    (130, 5, 40, 700, 200),   # lists shorter than a tile, and empty ones
+], ids=str)
+def test_forward_of_many_small_tiles(nq, nprobe, groups, n, k, pad, shift, dtype):
+    real = torch.float32 if dtype == torch.int8 else dtype
+    x, w, _, off, ids = _inputs((nq, nprobe, groups, n, k, 0.2, 0.05), real, 6)
+    lists = off.cuda(), ids.cuda(), nprobe
+    out, flat = _strided(torch.full((nq * nprobe, n), 7.0, dtype=real), pad, shift)
+    if dtype == torch.int8:
+        (cx, sx), (cw, sw) = codes64(x), codes64(w.reshape(-1, k))
+        cw, sw = cw.reshape(w.shape), sw.reshape(groups, n)
+        rabitq.grouped_matmul_i8(_strided(cx, pad, shift)[0], sx.cuda(), _strided(cw, pad, shift)[0], sw.cuda(), *lists, out=out)
+        want, named = grouped_i8_64(cx, sx, cw, sw, off, ids, nprobe)
+        assert_scaled(out[named], want[named], real)
+    else:
+        rabitq.grouped_matmul(_strided(x, pad, shift)[0], _strided(w, pad, shift)[0], *lists, out=out)
+        want, mag, named = forward64(x, w, off, ids, nprobe)
+        assert_sums(out[named], want[named], mag[named], k, dtype)
+    assert (out[~named] == 7.0).all()
+    assert _untouched(out, flat)
+
+
 def test_offsets_behind_32_bits():
     # rows that lie more than 2^31 elements apart, of every operand
     far = (1 << 31) + 64
