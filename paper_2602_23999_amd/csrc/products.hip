@@ -145,20 +145,31 @@ static int launch_few(const ProductArgs& p, hipStream_t st) {
   return RABITQ_OK;
 }
 
-// The edge of the tile.  A larger one moves fewer bytes per product (8192 x 8192 x 4096 codes: 521, 365, 277 us for 64, 128, 256), but
-// leaves the chip idle when there are few tiles (2048 x 4096 x 4096: 64, 46, 56; 1000 x 4096 x 4096: 33, 34, 53), multiplies rows
-// that are not there where lists are shorter than it (64 lists of 64 rows, 2048 x 2048 bf16: 150, 170, 182; of 128 rows: 200, 190,
-// 202; of 256 rows: 320, 252, 252), and has less to overlap its start and end with where the contraction is one or two steps
-// (10 000 x 1024 x 128 codes: 17, 21, 19).  For dw the rows and columns are those of the matrices and always there.
-static int tile_size(const ProductArgs& p, int op, int size) {
+// The edge of the tile.  A larger one moves fewer bytes per product, but fills the chip only with many rows and columns, and in rounds:
+// a compute unit has one tile of 256 at a time, two of 128, more of 64.  The estimates below are in the time of a round of 256 tiles of
+// 256.  A round that is not full saves half of what is missing (the card is limited by its power, and the others run faster); 512 tiles
+// of 128 take 0.6, 256 of 64 0.105 (8192 x 4096 x 1024 bf16, 2 rounds of 256: 71 us, 128: 85, 64: 118; 4352 x 4096 x 1024, a round and
+// a bit: 60, 56, 63; 2048 x 4096 x 4096 codes, half a round: 56, 46, 64; 8192 rows, 8 lists, 1024 x 2048 bf16, 144 tiles of 256, but 544
+// of 128: 53, 66, 72).  fp32 tiles are bound by the multiplication, so that their size hardly matters and what is left over at the end
+// does: 0.26 and 0.07 for 256 tiles (8192 x 4096 x 1024: 488, 504, 518 us; 4352 x 4096 x 1024: 481, 320, 294).
+// A list ends inside its last tile, half a tile behind its end on average; rows of lists shorter than a tile would be multiplied
+// for nothing (64 lists of 64 rows, 2048 x 2048 bf16: 182, 170, 150).  With one or two steps of contraction there is less to overlap
+// a tile's start and end with (10 000 x 1024 x 128 codes: 19, 21, 17).  For dw the rows and columns are those of the matrices.
+static int tile_size(const ProductArgs& p, int op, int size, bool fast) {
   const int64_t width = op == FORWARD ? p.n : p.k;
   const int64_t rows = op == GRAD_W ? p.n : p.pairs / p.groups;  // of a list, on average
   const int64_t lists = op == GRAD_W && p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups;
   const int64_t contraction = op == FORWARD ? p.k : op == GRAD_X ? p.n : p.part > 0 ? p.part : p.pairs / p.groups;
-  if (contraction * size < 512) return 64;
-  if (rows >= 256 && up(rows, 256) * up(width, 256) * lists >= 256) return 256;
-  if (rows >= 128 && up(rows, 128) * up(width, 128) * lists >= 512) return 128;
-  return 64;
+  if (contraction * size < 512 || rows < 128) return 64;
+  const auto rounds = [&](int64_t edge, int64_t round) {
+    const bool whole = op == GRAD_W || lists == 1;
+    const int64_t tiles = (whole ? up(rows, edge) * lists : p.pairs / edge + lists / 2) * up(width, edge);
+    return size == 4 ? (double)up(tiles, round) : ((double)tiles / (double)round + (double)up(tiles, round)) / 2;
+  };
+  const double of_64 = (size == 4 ? 0.07 : 0.105) * rounds(64, 256);
+  const double of_128 = size == 4 ? 0.26 * rounds(128, 256) : 0.6 * rounds(128, 512);
+  if (fast && rows >= 256 && rounds(256, 256) <= std::min(of_64, of_128)) return 256;
+  return of_128 <= of_64 ? 128 : 64;
 }
 
 // Whether four groups of wavefronts share a 64 x 64 tile of a forward or dx product: with little more than a tile for each compute unit,
@@ -175,9 +186,9 @@ static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
     if (few_rows(p, sizeof(T))) return launch_few<T>(p, st);
   }
-  const int edge = tile_size(p, OP, sizeof(T));
   const bool fast = fast_rows(p, OP, dtype);
-  if (edge == 256 && fast) return launch_tiles<T, OP, 256, 256, 2, 4, 1, true>(p, st);
+  const int edge = tile_size(p, OP, sizeof(T), fast);
+  if (edge == 256) return launch_tiles<T, OP, 256, 256, 2, 4, 1, true>(p, st);
   if (edge > 64)
     return fast ? launch_tiles<T, OP, 128, 128, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 128, 128, 2, 2, 1, false>(p, st);
   if constexpr (OP != GRAD_W) {

@@ -212,6 +212,33 @@ def test_large_products(rows, groups, odd, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,groups,wide,short", [
+    (4090, 1, 4096, 136),   # 256 tiles of 256 x 256, some not whole
+    (6100, 1, 4088, 136),   # 1536 tiles of 128 x 128
+    (8192, 4, 2048, 264),   # lists that end inside a tile of 256
+])
+def test_rounds_of_tiles(rows, groups, wide, short, dtype):
+    off, ids = lists_from(probes_of(rows, rows, 1, groups, 0, 0.02), groups)
+    lists = off.cuda(), ids.cuda(), 1
+    x, w = numbers(1, (rows, short), dtype).cuda(), numbers(2, (groups, wide, short), dtype).cuda()
+    want, mag, named = forward64(x, w, off, ids, 1)
+    got = rabitq.grouped_matmul(x, w, *lists, out=torch.full((rows, wide), 7.0, dtype=dtype, device="cuda"))
+    assert_sums(got[named], want[named], mag[named], short, dtype)
+    assert (got[~named] == 7.0).all()
+    w = numbers(3, (groups, short, wide), dtype).cuda()
+    want, mag, named = dx64(x, w, off, ids, 1)
+    got = rabitq.grouped_matmul_dx(x, w, *lists, out=torch.full((rows, wide), 7.0, dtype=dtype, device="cuda"))
+    assert_sums(got[named], want[named], mag[named], short, dtype)
+    assert (got[~named] == 7.0).all()
+    n, k = 4096 // groups, wide  # (dw of as many tiles, of few positions)
+    off, ids = lists_from(probes_of(5, 300, 1, groups, 0, 0.02), groups)
+    dy, x = numbers(4, (300, n), dtype).cuda(), numbers(5, (300, k), dtype).cuda()
+    want, mag = dw64(dy, x, off, ids, 1)
+    got = rabitq.grouped_matmul_dw(dy, x, off.cuda(), ids.cuda())
+    assert_sums(got, want, mag, int((off[1:] - off[:-1]).max()), dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("nq,nprobe,groups,wide,long", [
     (300, 2, 3, 130, 1100),
     (301, 1, 3, 129, 1111),     # rows that do not start at multiples of 16 bytes
