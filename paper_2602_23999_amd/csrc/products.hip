@@ -148,14 +148,14 @@ static int launch_few(const ProductArgs& p, hipStream_t st) {
 // The edge of the tile.  A larger one moves fewer bytes per product, but fills the chip only with many rows and columns, and in rounds:
 // a compute unit has one tile of 256 at a time, two of 128, more of 64.  The estimates below are in the time of a round of 256 tiles of
 // 256.  A round that is not full saves half of what is missing (the card is limited by its power, and the others run faster); 512 tiles
-// of 128 take 0.6, 256 of 64 0.105 (8192 x 4096 x 1024 bf16, 2 rounds of 256: 71 us, 128: 85, 64: 118; 4352 x 4096 x 1024, a round and
-// a bit: 60, 56, 63; 2048 x 4096 x 4096 codes, half a round: 56, 46, 64; 8192 rows, 8 lists, 1024 x 2048 bf16, 144 tiles of 256, but 544
-// of 128: 53, 66, 72).  fp32 tiles are bound by the multiplication, so that their size hardly matters and what is left over at the end
-// does: 0.26 and 0.07 for 256 tiles (8192 x 4096 x 1024: 488, 504, 518 us; 4352 x 4096 x 1024: 481, 320, 294).
-// A list ends inside its last tile, half a tile behind its end on average; rows of lists shorter than a tile would be multiplied
-// for nothing (64 lists of 64 rows, 2048 x 2048 bf16: 182, 170, 150).  With one or two steps of contraction there is less to overlap
-// a tile's start and end with (10 000 x 1024 x 128 codes: 19, 21, 17).  For dw the rows and columns are those of the matrices.
-static int tile_size(const ProductArgs& p, int op, int size, bool fast) {
+// of 128 take 0.6, 256 of 64 0.105 (8192 x 4096 x 1024 bf16, 2 rounds of 256: 71 us, 128: 85, 64: 118, rows at odd addresses 94 and 121;
+// 4352 x 4096 x 1024, a round and a bit: 60, 56, 63; 2048 x 4096 x 4096 codes, half a round: 56, 46, 64; 8192 rows, 8 lists, 1024 x 2048
+// bf16, 144 tiles of 256, but 544 of 128: 53, 66, 72).  fp32 tiles are bound by the multiplication, so that their size hardly matters
+// and what is left over at the end does: 0.26 and 0.07 for 256 tiles (8192 x 4096 x 1024: 488, 504, 518 us; 4352 x 4096 x 1024: 481,
+// 320, 294).  A list ends inside its last tile, half a tile behind its end on average; rows of lists shorter than a tile would be
+// multiplied for nothing (64 lists of 64 rows, 2048 x 2048 bf16: 182, 170, 150).  With one or two steps of contraction there is less
+// to overlap a tile's start and end with (10 000 x 1024 x 128 codes: 19, 21, 17).  For dw the rows and columns are those of the matrices.
+static int tile_size(const ProductArgs& p, int op, int size) {
   const int64_t width = op == FORWARD ? p.n : p.k;
   const int64_t rows = op == GRAD_W ? p.n : p.pairs / p.groups;  // of a list, on average
   const int64_t lists = op == GRAD_W && p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups;
@@ -168,7 +168,7 @@ static int tile_size(const ProductArgs& p, int op, int size, bool fast) {
   };
   const double of_64 = (size == 4 ? 0.07 : 0.105) * rounds(64, 256);
   const double of_128 = size == 4 ? 0.26 * rounds(128, 256) : 0.6 * rounds(128, 512);
-  if (fast && rows >= 256 && rounds(256, 256) <= std::min(of_64, of_128)) return 256;
+  if (rows >= 256 && rounds(256, 256) <= std::min(of_64, of_128)) return 256;
   return of_128 <= of_64 ? 128 : 64;
 }
 
@@ -187,8 +187,9 @@ static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
     if (few_rows(p, sizeof(T))) return launch_few<T>(p, st);
   }
   const bool fast = fast_rows(p, OP, dtype);
-  const int edge = tile_size(p, OP, sizeof(T), fast);
-  if (edge == 256) return launch_tiles<T, OP, 256, 256, 2, 4, 1, true>(p, st);
+  const int edge = tile_size(p, OP, sizeof(T));
+  if (edge == 256)
+    return fast ? launch_tiles<T, OP, 256, 256, 2, 4, 1, true>(p, st) : launch_tiles<T, OP, 256, 256, 2, 4, 1, false>(p, st);
   if (edge > 64)
     return fast ? launch_tiles<T, OP, 128, 128, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 128, 128, 2, 2, 1, false>(p, st);
   if constexpr (OP != GRAD_W) {

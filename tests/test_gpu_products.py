@@ -216,6 +216,9 @@ def test_large_products(rows, groups, odd, dtype):
     (4090, 1, 4096, 136),   # 256 tiles of 256 x 256, some not whole
     (6100, 1, 4088, 136),   # 1536 tiles of 128 x 128
     (8192, 4, 2048, 264),   # lists that end inside a tile of 256
+    (4090, 1, 4095, 135),   # the same, rows that do not start at multiples of 16 bytes
+    (6100, 1, 4081, 77),
+    (8192, 4, 2047, 263),
 ])
 def test_rounds_of_tiles(rows, groups, wide, short, dtype):
     off, ids = lists_from(probes_of(rows, rows, 1, groups, 0, 0.02), groups)
