@@ -172,13 +172,18 @@ static int tile_size(const ProductArgs& p, int op, int size) {
   return of_128 <= of_64 ? 128 : 64;
 }
 
-// Whether four groups of wavefronts share a 64 x 64 tile of a forward or dx product: with little more than a tile for each compute unit,
-// and 8 steps of contraction or more (256 x 4096 x 4096 codes, 256 tiles: 22 us, shared 14; 326 rows, 2 lists, 1222 x 7352 fp16:
-// 73 and 47; 2000 rows, 4 lists, 512 x 1024 bf16, 280 tiles: 13.6 and 14.2; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 20 and 28).
-static bool share_tiles(const ProductArgs& p, int op, int size) {
+// The rows of a tile of 64 columns that four groups of wavefronts share (forward and dx), or 0: with 8 steps of contraction or more, 32
+// where that gives no more than a tile for each compute unit (1119 rows, 5 of 10 lists each, 64 x 5472 fp32, 184 tiles: 56 us, 90 with
+// tiles of 64; 326 rows, 2 lists, 1222 x 7352 fp16, 240 tiles: 38 and 47; 300 x 2048 x 2048 fp16, 320 tiles: 19 and 13), 64 with little
+// more than a tile for each (256 x 4096 x 4096 codes, 256 tiles: 22 us, shared 14; 2000 rows, 4 lists, 512 x 1024 bf16, 280 tiles:
+// 13.6 and 14.2; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 20 and 28).
+static int shared_rows(const ProductArgs& p, int op, int size) {
   const int64_t width = op == FORWARD ? p.n : p.k, contraction = op == FORWARD ? p.k : p.n;
-  const int64_t rows = std::min<int64_t>(p.pairs, p.pair_off ? p.pairs / 64 + p.groups : up(p.pairs, 64));
-  return contraction * size >= 8 * 128 && rows * up(width, 64) <= 280;
+  if (contraction * size < 8 * 128) return 0;
+  const auto tiles = [&](int64_t rows) {
+    return std::min<int64_t>(p.pairs, p.pair_off ? p.pairs / rows + p.groups : up(p.pairs, rows)) * up(width, 64);
+  };
+  return tiles(32) <= 256 ? 32 : tiles(64) <= 280 ? 64 : 0;
 }
 
 template <class T, int OP>
@@ -193,7 +198,10 @@ static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if (edge > 64)
     return fast ? launch_tiles<T, OP, 128, 128, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 128, 128, 2, 2, 1, false>(p, st);
   if constexpr (OP != GRAD_W) {
-    if (share_tiles(p, OP, sizeof(T)))
+    const int rows = shared_rows(p, OP, sizeof(T));
+    if (rows == 32)
+      return fast ? launch_tiles<T, OP, 32, 64, 1, 2, 4, true>(p, st) : launch_tiles<T, OP, 32, 64, 1, 2, 4, false>(p, st);
+    if (rows == 64)
       return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 4, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 4, false>(p, st);
   }
   return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 1, false>(p, st);

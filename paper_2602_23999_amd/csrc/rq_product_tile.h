@@ -219,7 +219,9 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
   const char* pa[FAST ? 1 : NA];
   uint32_t oa[FAST && !TA ? NA : 1], ob[FAST && !TA ? NB : 1];
   const int line = tid >> 3;
-  const uint32_t ca = ((tid & 7) ^ swizzle_i(line)) * EPC, cb = ((tid & 7) ^ swizzle_j(line)) * EPC;  // (the same for all q)
+  const uint32_t ca = ((tid & 7) ^ swizzle_i(line)) * EPC;  // (the same for all q: NT / 8 lines on, of which it takes bits 1 to 3)
+  static_assert(NT % 128 == 0);
+  auto cb = [&](int q) -> uint32_t { return ((tid & 7) ^ swizzle_j(line) ^ swizzle_j(q * (NT / 8))) * EPC; };  // (takes bits 1, 2 and 4)
   constexpr int PA = BI * SZ / 16, PB = BJ * SZ / 16;     // pieces of a line of a turned operand
   if constexpr (!TA) {
 #pragma unroll
@@ -231,14 +233,14 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
     }
   }
   const char* pb = nullptr;  // piece 0; the others lie whole lines behind it
-  if constexpr (!FAST && !TB) pb = b + ((j0 + line) * p.ldb + cb) * SZ;
+  if constexpr (!FAST && !TB) pb = b + (j0 + line) * p.ldb * SZ;
   if constexpr (!FAST && OP == GRAD_X) pb = b + (tid / PB * p.ldb + j0) * SZ;
   if constexpr (FAST && !TA) {  // (rows and columns that are not there read the first ones, unused)
 #pragma unroll
     for (int q = 0; q < NB; ++q) {
       if constexpr (!TB) {
         const int row = line + q * (NT / 8);
-        ob[q] = (uint32_t)(((row < jleft ? row : 0) * p.ldb + cb) * SZ);
+        ob[q] = (uint32_t)(((row < jleft ? row : 0) * p.ldb + cb(q)) * SZ);
       } else {
         const int c = (tid + q * NT) / PB, col = swizzle_turned<SZ, PB>(c, (tid + q * NT) % PB) * EPC;
         ob[q] = (uint32_t)((c * p.ldb + (col < jleft ? col : 0)) * SZ);
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
       if (c0 + STEP <= nc) {
         load_to_lds(base, offset, at);
       } else {  // the last step: zeros behind the end
-        const uint32_t c = c0 + (q < NA ? ca : !TB ? cb : (uint32_t)(tid + qb * NT) / PB);
+        const uint32_t c = c0 + (q < NA ? ca : !TB ? cb(qb) : (uint32_t)(tid + qb * NT) / PB);
         load_to_lds(c < nc ? base + offset : zeros, at);
       }
     }
@@ -330,8 +332,8 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
   };
   auto piece_b = [&](int q, uint32_t c0, const char*& from) -> int {
     if constexpr (!TB) {
-      from = pb + ((int64_t)(q * (NT / 8)) * p.ldb + c0) * SZ;
-      return line + q * (NT / 8) < jleft && c0 + cb < nc ? (int)(nc - c0 - cb) : 0;
+      from = pb + ((int64_t)(q * (NT / 8)) * p.ldb + c0 + cb(q)) * SZ;
+      return line + q * (NT / 8) < jleft && c0 + cb(q) < nc ? (int)(nc - c0 - cb(q)) : 0;
     } else if constexpr (OP == GRAD_X) {
       const int c = (tid + q * NT) / PB, piece = swizzle_turned<SZ, PB>(c, (tid + q * NT) % PB);
       from = pb + ((int64_t)(c0 + q * (NT / PB)) * p.ldb + piece * EPC) * SZ - back_b;

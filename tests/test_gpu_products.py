@@ -248,6 +248,8 @@ def test_rounds_of_tiles(rows, groups, wide, short, dtype):
     (200, 1, 1, 64, 520),       # of four parts of the contraction the last is empty (16-bit types)
     (200, 1, 1, 64, 263),       # ... (f32), and one ends inside a step
     (700, 1, 2, 72, 8200),
+    (2200, 1, 1, 150, 1104),    # more than 512 tiles of 16 x 16, fewer than 256 of 32 x 64
+    (1100, 3, 3, 80, 1041),
 ], ids=str)
 def test_few_tiles_of_a_long_contraction(nq, nprobe, groups, wide, long, dtype):
     off, ids = lists_from(probes_of(nq, nq, nprobe, groups, 0, 0.05), groups)
