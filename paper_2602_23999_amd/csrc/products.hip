@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void sum_named_kernel(const float* __restrict_
 
 static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
-template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, bool FAST>
+template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, int STEPS, bool FAST>
 static int launch_tiles(ProductArgs p, hipStream_t st) {
   const int64_t width = OP == FORWARD ? p.n : p.k;
   p.tiles_i = OP == GRAD_W ? up(p.n, BI) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups)
@@ -97,8 +97,8 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
-  const size_t lds = KS * 2 * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int2) : BI * (sizeof(int) + sizeof(float)));
-  auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, KS, FAST>;
+  const size_t lds = KS * STEPS * (BI + BJ) * 128 + (OP == GRAD_W ? 1024 * sizeof(int2) : BI * (sizeof(int) + sizeof(float)));
+  auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, KS, STEPS, FAST>;
   if (p.check_only) return RABITQ_OK;
   if (lds > 64 * 1024) RQ_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
   kernel<<<(unsigned)grid, 64 * WI * WJ * KS, lds, st>>>(p);
@@ -174,9 +174,9 @@ static int tile_size(const ProductArgs& p, int op, int size) {
 
 // The rows of a tile of 64 columns that four groups of wavefronts share (forward and dx), or 0: with 8 steps of contraction or more, 32
 // where that gives no more than a tile for each compute unit (1119 rows, 5 of 10 lists each, 64 x 5472 fp32, 184 tiles: 56 us, 90 with
-// tiles of 64; 326 rows, 2 lists, 1222 x 7352 fp16, 240 tiles: 38 and 47; 300 x 2048 x 2048 fp16, 320 tiles: 19 and 13), 64 with little
-// more than a tile for each (256 x 4096 x 4096 codes, 256 tiles: 22 us, shared 14; 2000 rows, 4 lists, 512 x 1024 bf16, 280 tiles:
-// 13.6 and 14.2; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 20 and 28).
+// tiles of 64; 326 rows, 2 lists, 1222 x 7352 fp16, 240 tiles: 32, with two steps in LDS 39, and 47; 300 x 2048 x 2048 fp16, 320 tiles:
+// 19 and 13), 64 with little more than a tile for each (256 x 4096 x 4096 codes, 256 tiles: 22 us, shared 14; 2000 rows, 4 lists,
+// 512 x 1024 bf16, 280 tiles: 13.6 and 14.2; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 20 and 28).
 static int shared_rows(const ProductArgs& p, int op, int size) {
   const int64_t width = op == FORWARD ? p.n : p.k, contraction = op == FORWARD ? p.k : p.n;
   if (contraction * size < 8 * 128) return 0;
@@ -186,6 +186,12 @@ static int shared_rows(const ProductArgs& p, int op, int size) {
   return tiles(32) <= 256 ? 32 : tiles(64) <= 280 ? 64 : 0;
 }
 
+// Whether the lists are shorter than a tile of 64, so that the matrices, read once each, are what the time goes to: a third step on its
+// way is worth more than a fourth workgroup per compute unit (64 lists of 32 rows, 1024 x 2048 bf16: 91 us with two steps, 72 with
+// three, codes 44 and 36; of 64 rows, 2048 x 2048 bf16: 184 and 164; but 1000 x 4096 x 4096 bf16 52 and 60).  fp32 tiles, bound by the
+// multiplication, would rather have the workgroup (64 lists of 64 rows, 2048 x 2048: 456 and 496).
+static bool short_lists(const ProductArgs& p) { return p.pairs <= 64 * (int64_t)p.groups; }
+
 template <class T, int OP>
 static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
@@ -194,17 +200,20 @@ static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   const bool fast = fast_rows(p, OP, dtype);
   const int edge = tile_size(p, OP, sizeof(T));
   if (edge == 256)
-    return fast ? launch_tiles<T, OP, 256, 256, 2, 4, 1, true>(p, st) : launch_tiles<T, OP, 256, 256, 2, 4, 1, false>(p, st);
-  if (edge > 64)
-    return fast ? launch_tiles<T, OP, 128, 128, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 128, 128, 2, 2, 1, false>(p, st);
+    return fast ? launch_tiles<T, OP, 256, 256, 2, 4, 1, 2, true>(p, st) : launch_tiles<T, OP, 256, 256, 2, 4, 1, 2, false>(p, st);
+  if (edge == 128)
+    return fast ? launch_tiles<T, OP, 128, 128, 2, 2, 1, 2, true>(p, st) : launch_tiles<T, OP, 128, 128, 2, 2, 1, 2, false>(p, st);
   if constexpr (OP != GRAD_W) {
     const int rows = shared_rows(p, OP, sizeof(T));
     if (rows == 32)
-      return fast ? launch_tiles<T, OP, 32, 64, 1, 2, 4, true>(p, st) : launch_tiles<T, OP, 32, 64, 1, 2, 4, false>(p, st);
+      return fast ? launch_tiles<T, OP, 32, 64, 1, 2, 4, 3, true>(p, st) : launch_tiles<T, OP, 32, 64, 1, 2, 4, 2, false>(p, st);
     if (rows == 64)
-      return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 4, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 4, false>(p, st);
+      return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 4, 2, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 4, 2, false>(p, st);
+    if constexpr (sizeof(T) < 4) {
+      if (fast && short_lists(p)) return launch_tiles<T, OP, 64, 64, 2, 2, 1, 3, true>(p, st);
+    }
   }
-  return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 1, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 1, false>(p, st);
+  return fast ? launch_tiles<T, OP, 64, 64, 2, 2, 1, 2, true>(p, st) : launch_tiles<T, OP, 64, 64, 2, 2, 1, 2, false>(p, st);
 }
 
 template <int OP>

@@ -69,9 +69,12 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, u
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
 }
 // (As builtins and not in the asm, so that the compiler's own count of LDS reads in flight starts again from none.)
-__device__ __forceinline__ void wait_and_barrier() {
+template <int LATER>  // loads of this wavefront that may still be on their way, if some_later
+__device__ __forceinline__ void wait_and_barrier(bool some_later) {
+  static_assert(LATER < 16);
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  if (LATER > 0 && some_later) __builtin_amdgcn_s_waitcnt(0x0070 | LATER);  // vmcnt(LATER) lgkmcnt(0)
+  else __builtin_amdgcn_s_waitcnt(0x0070);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -126,7 +129,9 @@ static __device__ __align__(16) unsigned char product_zeros[16];
 //
 // KS: groups of wavefronts that share a tile, each with its own part of the contraction and its own steps in LDS; their sums are added
 // up in order at the end.  For long contractions of so few tiles that most of the chip would be idle.
-template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, bool FAST>
+//
+// STEPS: steps in LDS, the one that is multiplied and those on their way: 2, or (FAST) 3 where a step is over before the next has come.
+template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, int STEPS, bool FAST>
 __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(ProductArgs p) {
   constexpr int NT = 64 * WI * WJ, SZ = sizeof(T), EPC = 16 / SZ, STEP = 128 / SZ;
   constexpr bool TA = OP == GRAD_W, TB = OP != FORWARD;
@@ -134,11 +139,11 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
   constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;     // 32 x 32 products per wavefront
   constexpr int STAGE = (BI + BJ) * 128;
   using Acc = typename Mma<T>::Acc;
-  static_assert(KS == 1 || !TA);
+  static_assert((KS == 1 || !TA) && (STEPS == 2 || (STEPS == 3 && FAST)));
   extern __shared__ __align__(16) char smem_all[];
   const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ks = wave_all / (WI * WJ);
-  char* smem = smem_all + ks * (2 * STAGE);
-  int* row_pair = reinterpret_cast<int*>(smem_all + KS * 2 * STAGE);  // [BI] pair of every row, or -1
+  char* smem = smem_all + ks * (STEPS * STAGE);
+  int* row_pair = reinterpret_cast<int*>(smem_all + KS * STEPS * STAGE);  // [BI] pair of every row, or -1
   float* row_scale = reinterpret_cast<float*>(row_pair + BI);  // [BI] codes only
   int2* block_pairs = reinterpret_cast<int2*>(row_pair);     // dw: [2][512] pairs of the positions and their rows of x, or -1
   const int tid = threadIdx.x % NT, lane = tid & 63, wave = wave_all % (WI * WJ);  // of the group
@@ -424,10 +429,9 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
     for (int y = 0; y < FJ; ++y) acc[x][y] = Acc{0};
 
   // A step is multiplied in four parts of 32 bytes of every line; the operands of the next part are read while one is multiplied.
-  // The one barrier of a step stands in front of its last part, where everybody has read the whole step and the next one, requested
-  // a step ago, has arrived; behind it the step after that is requested into the half that is free, one half of its pieces during
-  // that part and the other during the next.  Reads and requests are dealt out among the products.  Behind the last step the reads go
-  // on for nothing (old lines of LDS).
+  // The one barrier of a step stands in front of its last part, where everybody has read the whole step and the next one has
+  // arrived; behind it the step that takes its place in LDS is requested, one half of its pieces during that part and the other during
+  // the next.  Reads and requests are dealt out among the products.  Behind the last step the reads go on for nothing (old lines of LDS).
   i32x4 ai[2][FI], bj[2][FJ];
   auto read_one = [&](const char* st, int r, int sub, int set) {
     if (r < FJ) bj[set][r < FJ ? r : 0] = frag_j(st, r < FJ ? r : 0, sub);
@@ -478,34 +482,41 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
       store_block(1);
       __syncthreads();
     }
-    find_pairs(0);
-    fetch_all(0, 0);
-    find_pairs(STEP);
+#pragma unroll
+    for (int u = 0; u < STEPS - 1; ++u) {
+      find_pairs(u * STEP);
+      fetch_all(u * STEP, u);
+    }
+    find_pairs((STEPS - 1) * STEP);
     stash(0);
-    wait_and_barrier();
+    constexpr int LATER = (STEPS - 2) * (NA + NB);
+    wait_and_barrier<LATER>(STEP < span);
 #pragma unroll
     for (int r = 0; r < FI + FJ; ++r) read_one(smem, r, 0, 0);
     if constexpr (FAST) {
 #pragma unroll
       for (int q = 0; q < NA + NB; ++q)
-        if (q * (2 * FI) / (NA + NB) < FI) fetch_piece(q, STEP, 1);
+        if (q * (2 * FI) / (NA + NB) < FI) fetch_piece(q, (STEPS - 1) * STEP, STEPS - 1);
     } else {
       fetch_regs(STEP);
     }
     int buf = 0;
-    for (uint32_t c0 = 0; c0 < span; c0 += STEP, buf ^= 1) {
+    for (uint32_t c0 = 0; c0 < span; c0 += STEP) {
       // (the first step of block b: nobody looks at block b - 1 any more, and b + 1 is there)
       const bool refill = TA && c0 != 0 && c0 % BLOCK == 0;
-      multiply(sub0, buf, second, c0 + STEP, buf ^ 1);
+      const int next = STEPS == 2 ? buf ^ 1 : buf == STEPS - 1 ? 0 : buf + 1;
+      const int before = STEPS == 2 ? next : buf == 0 ? STEPS - 1 : buf - 1;
+      multiply(sub0, buf, second, c0 + (STEPS - 1) * STEP, before);
       if (refill) load_block(c0 / BLOCK + 1);
       multiply(sub1, buf, nothing, 0, 0);
-      find_pairs(c0 + 2 * STEP);
+      find_pairs(c0 + STEPS * STEP);
       multiply(sub2, buf, nothing, 0, 0);
-      stash(buf ^ 1);
-      wait_and_barrier();
+      stash(next);
+      wait_and_barrier<LATER>(c0 + 2 * STEP < span);  // (then the step after the next was requested behind the next)
       if (refill) store_block(c0 / BLOCK + 1);
       if constexpr (!FAST) fetch_regs(c0 + 2 * STEP);
-      multiply(sub3, buf ^ 1, first, c0 + 2 * STEP, buf);
+      multiply(sub3, next, first, c0 + STEPS * STEP, buf);
+      buf = next;
     }
     __builtin_amdgcn_s_waitcnt(0x0070);  // nothing may be on its way to LDS when the workgroup ends
   }

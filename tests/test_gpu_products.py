@@ -388,6 +388,7 @@ def test_strides_and_alignment_of_codes(m, n, k, pad, shift):
     (600, 1, 2, 1000, 1120),  # few tiles of 64 x 64 of a long contraction, but many of 16 x 16
     (600, 1, 2, 1001, 1111),
     (130, 5, 40, 700, 200),   # lists shorter than a tile, and empty ones
+    (200, 8, 48, 720, 1040),
 ], ids=str)
 def test_forward_of_many_small_tiles(nq, nprobe, groups, n, k, pad, shift, dtype):
     real = torch.float32 if dtype == torch.int8 else dtype
@@ -404,6 +405,19 @@ def test_forward_of_many_small_tiles(nq, nprobe, groups, n, k, pad, shift, dtype
         rabitq.grouped_matmul(_strided(x, pad, shift)[0], _strided(w, pad, shift)[0], *lists, out=out)
         want, mag, named = forward64(x, w, off, ids, nprobe)
         assert_sums(out[named], want[named], mag[named], k, dtype)
+    assert (out[~named] == 7.0).all()
+    assert _untouched(out, flat)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("pad,shift", [(0, 0), (1, 0)])
+@pytest.mark.parametrize("nq,nprobe,groups,n,k", [(1100, 2, 3, 272, 1032), (200, 8, 48, 1040, 720), (130, 5, 40, 200, 700)], ids=str)
+def test_dx_of_many_small_tiles(nq, nprobe, groups, n, k, pad, shift, dtype):
+    _, w, dy, off, ids = _inputs((nq, nprobe, groups, n, k, 0.2, 0.05), dtype, 7)
+    out, flat = _strided(torch.full((nq, k), 7.0, dtype=dtype), pad, shift)
+    rabitq.grouped_matmul_dx(_strided(dy, pad, shift)[0], _strided(w, pad, shift)[0], off.cuda(), ids.cuda(), nprobe, out=out)
+    want, mag, named = dx64(dy, w, off, ids, nprobe)
+    assert_sums(out[named], want[named], mag[named], n * nprobe, dtype)
     assert (out[~named] == 7.0).all()
     assert _untouched(out, flat)
 
