@@ -415,6 +415,7 @@ def _output(out, shape, dtype, like, dev: int, what="out"):
     """(tensor, address, row stride, matrix stride) of the caller's output, or of a new one on the device of `like`."""
     if out is None:
         out = like.new_empty(shape, dtype=dtype)
+        return out, out.data_ptr(), shape[-1], shape[-1] * shape[1] if len(shape) == 3 else 0
     ptr, have, ld, stride = _operand(out, dtype, len(shape), what, dev)
     if have != shape:
         raise RabitqError(f"{what}: expected the shape {tuple(shape)}, got {tuple(have)}")
@@ -516,8 +517,10 @@ def quantize_rows(x, codes=None, scale=None):
     codes, pc, ldc, _ = _output(codes, (rows, k), torch.int8, x, dev, "codes")
     if scale is None:
         scale = x.new_empty(rows, dtype=torch.float32)
-    _check(load_library().rabitq_quantize_rows(px, DTYPES[dt], ldx, rows, _int32(k, "elements of a row"), pc, ldc,
-                                               _vector(scale, torch.float32, (rows,), "scale", dev),
+        ps = scale.data_ptr()
+    else:
+        ps = _vector(scale, torch.float32, (rows,), "scale", dev)
+    _check(load_library().rabitq_quantize_rows(px, DTYPES[dt], ldx, rows, _int32(k, "elements of a row"), pc, ldc, ps,
                                                torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale
 
