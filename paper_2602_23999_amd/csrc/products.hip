@@ -82,18 +82,30 @@ __global__ __launch_bounds__(256) void sum_named_kernel(const float* __restrict_
 
 static int64_t up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
+struct TileGrid {
+  int64_t tiles_i, strips, strip, workgroups;
+  bool fits(int threads) const { return workgroups <= MAX_GRID / threads; }
+};
+static TileGrid grid_of(const ProductArgs& p, int op, int64_t bi, int64_t bj) {
+  TileGrid g;
+  const int64_t width = op == FORWARD ? p.n : p.k;
+  g.tiles_i = op == GRAD_W ? up(p.n, bi) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups)
+                           : p.pair_off ? p.pairs / bi + p.groups : up(p.pairs, bi);
+  // strips of up to 8 tiles, evenly dealt out; shorter where that would be less than 16 for each XCD
+  const int64_t tiles_j = up(width, bj), most = std::min<int64_t>(8, std::max<int64_t>(1, g.tiles_i * tiles_j / 128));
+  g.strips = up(tiles_j, most);
+  g.strip = up(tiles_j, g.strips);
+  g.workgroups = up(g.tiles_i * g.strips, 8) * 8 * g.strip;
+  return g;
+}
+
 template <class T, int OP, int BI, int BJ, int WI, int WJ, int KS, int STEPS, bool FAST>
 static int launch_tiles(ProductArgs p, hipStream_t st) {
-  const int64_t width = OP == FORWARD ? p.n : p.k;
-  p.tiles_i = OP == GRAD_W ? up(p.n, BI) * (p.part > 0 ? dw_parts(p.pairs, p.groups, p.part) : p.groups)
-                           : p.pair_off ? p.pairs / BI + p.groups : up(p.pairs, BI);
-  // strips of up to 8 tiles, evenly dealt out; shorter where that would be less than 16 for each XCD
-  const int64_t tiles_j = up(width, BJ), most = std::min<int64_t>(8, std::max<int64_t>(1, p.tiles_i * tiles_j / 128));
-  const int64_t strips = up(tiles_j, most), strip = up(tiles_j, strips);
-  p.strips = (uint32_t)strips;
-  p.strip = (uint32_t)strip;
-  const int64_t grid = up(p.tiles_i * strips, 8) * 8 * strip;
-  if (grid > MAX_GRID / (64 * WI * WJ * KS)) {
+  const TileGrid grid = grid_of(p, OP, BI, BJ);
+  p.tiles_i = grid.tiles_i;
+  p.strips = (uint32_t)grid.strips;
+  p.strip = (uint32_t)grid.strip;
+  if (!grid.fits(64 * WI * WJ * KS)) {
     set_error("too many tiles of work");
     return RABITQ_EINVAL;
   }
@@ -101,7 +113,7 @@ static int launch_tiles(ProductArgs p, hipStream_t st) {
   auto kernel = product_tile_kernel<T, OP, BI, BJ, WI, WJ, KS, STEPS, FAST>;
   if (p.check_only) return RABITQ_OK;
   if (lds > 64 * 1024) RQ_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  kernel<<<(unsigned)grid, 64 * WI * WJ * KS, lds, st>>>(p);
+  kernel<<<(unsigned)grid.workgroups, 64 * WI * WJ * KS, lds, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }
@@ -133,14 +145,11 @@ static bool few_rows(const ProductArgs& p, int size) {
   return tiles16 <= (size == 4 ? 1024 : 512) * up(tiles64, 256);
 }
 
+static int64_t few_workgroups(const ProductArgs& p) { return (p.pair_off ? p.pairs / 16 + p.groups : up(p.pairs, 16)) * up(p.n, 16); }
+
 template <class T>
 static int launch_few(const ProductArgs& p, hipStream_t st) {
-  const int64_t grid = (p.pair_off ? p.pairs / 16 + p.groups : up(p.pairs, 16)) * up(p.n, 16);
-  if (grid > MAX_GRID / 256) {
-    set_error("too many tiles of work");
-    return RABITQ_EINVAL;
-  }
-  product_few_kernel<T><<<(unsigned)grid, 256, 0, st>>>(p);
+  product_few_kernel<T><<<(unsigned)few_workgroups(p), 256, 0, st>>>(p);
   RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }
@@ -192,13 +201,17 @@ static int shared_rows(const ProductArgs& p, int op, int size) {
 // multiplication, would rather have the workgroup (64 lists of 64 rows, 2048 x 2048: 456 and 496).
 static bool short_lists(const ProductArgs& p) { return p.pairs <= 64 * (int64_t)p.groups; }
 
+// A launch holds fewer than 2^32 threads, which few rows (of x or of each list) against many columns can pass: 256 threads take 16 columns
+// in the kernel for few rows, 64 in tiles of 64, 128 in tiles of 128.  Where the one that the rules above choose does not hold the work,
+// the next does (one query against 2^28 rows and more; 2^20 lists of 512 columns).
 template <class T, int OP>
 static int launch_typed(const ProductArgs& p, int dtype, hipStream_t st) {
   if constexpr (OP == FORWARD) {
-    if (few_rows(p, sizeof(T))) return launch_few<T>(p, st);
+    if (few_rows(p, sizeof(T)) && few_workgroups(p) <= MAX_GRID / 256) return launch_few<T>(p, st);
   }
   const bool fast = fast_rows(p, OP, dtype);
-  const int edge = tile_size(p, OP, sizeof(T));
+  int edge = tile_size(p, OP, sizeof(T));
+  if (edge == 64 && !grid_of(p, OP, 64, 64).fits(256)) edge = 128;
   if (edge == 256)
     return fast ? launch_tiles<T, OP, 256, 256, 2, 4, 1, 2, true>(p, st) : launch_tiles<T, OP, 256, 256, 2, 4, 1, 2, false>(p, st);
   if (edge == 128)
