@@ -13,6 +13,7 @@ import os
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librabitq_hip.so")
@@ -372,7 +373,8 @@ class Index:
 
 # ---- products by list and products of 8-bit integers -------------------------------
 # Plain calls on tensors of the current device: strided rows are taken as they are, nothing is copied, and no gradient is
-# recorded (grouped_matmul_dx and grouped_matmul_dw are the backward pass).
+# recorded (grouped_matmul_dx and grouped_matmul_dw are the backward pass) and no tangent carried on: tensors that ask for
+# either are refused.
 
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
@@ -387,6 +389,8 @@ def _operand(t, dtype, dims: int, what: str, dev: int):
     if t.requires_grad and torch.is_grad_enabled():
         raise RabitqError(f"{what} requires a gradient, which this call does not record: pass it detached or under "
                           "torch.no_grad()")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise RabitqError(f"{what} carries a tangent, which this call does not carry on: pass its primal")
     shape = t.shape
     if t.is_contiguous():
         ld = shape[-1]
