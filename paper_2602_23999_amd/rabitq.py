@@ -14,6 +14,7 @@ import os
 import numpy as np
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.graph import increment_version
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librabitq_hip.so")
@@ -426,6 +427,14 @@ def _output(out, shape, dtype, like, dev: int, what="out"):
     return out, ptr, ld, stride
 
 
+def _written(*outputs) -> None:
+    """Tells automatic differentiation that the caller's outputs (None: not given) have new values, as torch's own calls do: a
+    backward pass that saved one of them refuses to use it."""
+    for t in outputs:
+        if t is not None:
+            increment_version(t)
+
+
 def _vector(t, dtype, shape, what: str, dev: int) -> int:
     ptr, have, _, _ = _operand(t, dtype, len(shape), what, dev)
     if have != shape or not t.is_contiguous():
@@ -468,9 +477,11 @@ def grouped_matmul(x, w, pair_off, pair_ids=None, nprobe: int = 1, out=None):
     if kw != k:
         raise RabitqError(f"rows of x have {k} elements, those of w {kw}")
     ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids, dev)
+    given = out
     out, po, ldo, _ = _output(out, (nq * nprobe, n), dt, x, dev)
     _check(load_library().rabitq_grouped_matmul(C.byref(ls), DTYPES[dt], px, ldx, pw, ldw, stride_w, po, ldo,
                                                 torch._C._cuda_getCurrentRawStream(dev)))
+    _written(given)
     return out
 
 
@@ -485,12 +496,14 @@ def grouped_matmul_dx(dout, w, pair_off, pair_ids=None, nprobe: int = 1, out=Non
     if pairs % nprobe:
         raise RabitqError("dout must have nprobe rows per row of x")
     ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids, dev)
+    given = out
     out, po, ldo, _ = _output(out, (pairs // nprobe, k), dt, dout, dev)
     lib = load_library()
     scratch = _scratch(lib.rabitq_grouped_dx_scratch_bytes(C.byref(ls)), dout)
     _check(lib.rabitq_grouped_matmul_dx(C.byref(ls), DTYPES[dt], pd, ldd, pw, ldw, stride_w, po, ldo,
                                         None if scratch is None else scratch.data_ptr(),
                                         torch._C._cuda_getCurrentRawStream(dev)))
+    _written(given)
     return out
 
 
@@ -504,12 +517,14 @@ def grouped_matmul_dw(dout, x, pair_off, pair_ids=None, nprobe: int = 1, out=Non
         raise RabitqError(f"dout must have {nq * nprobe} rows, got {pairs}")
     g = _operand(pair_off, torch.int32, 1, "pair_off", dev)[1][0] - 1
     ls = _lists_of(g, n, k, pairs, nprobe, pair_off, pair_ids, dev)
+    given = out
     out, po, ldo, stride = _output(out, (g, n, k), dt, dout, dev)
     lib = load_library()
     scratch = _scratch(lib.rabitq_grouped_dw_scratch_bytes(C.byref(ls)), dout)
     _check(lib.rabitq_grouped_matmul_dw(C.byref(ls), DTYPES[dt], pd, ldd, px, ldx, po, ldo, stride,
                                         None if scratch is None else scratch.data_ptr(),
                                         torch._C._cuda_getCurrentRawStream(dev)))
+    _written(given)
     return out
 
 
@@ -518,6 +533,7 @@ def quantize_rows(x, codes=None, scale=None):
     x about codes * scale[:, None]."""
     dt, dev = _float_type(x, "x"), _current_device(x)
     px, (rows, k), ldx, _ = _operand(x, dt, 2, "x", dev)
+    given = codes, scale
     codes, pc, ldc, _ = _output(codes, (rows, k), torch.int8, x, dev, "codes")
     if scale is None:
         scale = x.new_empty(rows, dtype=torch.float32)
@@ -526,6 +542,7 @@ def quantize_rows(x, codes=None, scale=None):
         ps = _vector(scale, torch.float32, (rows,), "scale", dev)
     _check(load_library().rabitq_quantize_rows(px, DTYPES[dt], ldx, rows, _int32(k, "elements of a row"), pc, ldc, ps,
                                                torch._C._cuda_getCurrentRawStream(dev)))
+    _written(*given)
     return codes, scale
 
 
@@ -538,11 +555,13 @@ def matmul_i8(a, scale_a, b, scale_b, out_dtype=torch.float32, out=None):
         raise RabitqError(f"rows of a have {k} elements, those of b {kb}")
     if out_dtype not in DTYPES:
         raise RabitqError("out_dtype must be float32, float16 or bfloat16")
+    given = out
     out, po, ldo, _ = _output(out, (m, n), out_dtype, a, dev)
     _check(load_library().rabitq_matmul_i8(pa, lda, _vector(scale_a, torch.float32, (m,), "scale_a", dev), pb, ldb,
                                            _vector(scale_b, torch.float32, (n,), "scale_b", dev), m, n,
                                            _int32(k, "elements of a row"), po,
                                            DTYPES[out_dtype], ldo, torch._C._cuda_getCurrentRawStream(dev)))
+    _written(given)
     return out
 
 
@@ -557,11 +576,13 @@ def grouped_matmul_i8(x, scale_x, w, scale_w, pair_off, pair_ids=None, nprobe: i
     if out_dtype not in DTYPES:
         raise RabitqError("out_dtype must be float32, float16 or bfloat16")
     ls = _lists_of(g, n, k, nq * nprobe, nprobe, pair_off, pair_ids, dev)
+    given = out
     out, po, ldo, _ = _output(out, (nq * nprobe, n), out_dtype, x, dev)
     _check(load_library().rabitq_grouped_matmul_i8(
         C.byref(ls), px, ldx, _vector(scale_x, torch.float32, (nq,), "scale_x", dev), pw, ldw, stride_w,
         _vector(scale_w, torch.float32, (g, n), "scale_w", dev), po, DTYPES[out_dtype], ldo,
         torch._C._cuda_getCurrentRawStream(dev)))
+    _written(given)
     return out
 
 
