@@ -387,6 +387,8 @@ def _operand(t, dtype, dims: int, what: str, dev: int):
         raise RabitqError(f"{what}: expected a tensor on the current CUDA device")
     if t.dtype is not dtype or t.dim() != dims:
         raise RabitqError(f"{what}: expected {dims} dimensions of {dtype}, got {t.dim()} of {t.dtype}")
+    if t.is_neg():  # (the imaginary part of a conjugate: memory holds the numbers with the other sign)
+        raise RabitqError(f"{what} is a view with its sign turned: pass it resolved (resolve_neg)")
     if t.requires_grad and torch.is_grad_enabled():
         raise RabitqError(f"{what} requires a gradient, which this call does not record: pass it detached or under "
                           "torch.no_grad()")

@@ -43,3 +43,12 @@ def test_tensors_that_carry_a_tangent():
             with torch.no_grad(), pytest.raises(rabitq.RabitqError, match="tangent"):
                 _operand(t)
         assert _operand(forward_ad.unpack_dual(dual).primal)[1] == (4, 6)
+
+
+def test_views_with_their_sign_turned():
+    # the only such views of floats that torch makes have stride 2, which rows of one element pass
+    z = torch.complex(torch.zeros(4, 1), torch.ones(4, 1)).conj().imag
+    assert z.is_neg() and z.stride() == (2, 2) and (z == -1).all()
+    with pytest.raises(rabitq.RabitqError, match="sign"):
+        _operand(z.as_subclass(_OnDevice))
+    assert _operand(z.resolve_neg().as_subclass(_OnDevice))[1] == (4, 1)
