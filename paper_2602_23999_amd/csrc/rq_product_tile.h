@@ -60,13 +60,14 @@ struct Mma<int8_t> {
 __device__ __forceinline__ int j_of_row(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
 // 16 bytes per lane from memory to LDS without registers: lane l's go to lds + 16 l.  Not waited for by the compiler: the kernel
-// waits for all of them in front of the barrier behind which they are read.
+// waits for all of them in front of the barrier behind which they are read.  The address in LDS goes through m0, as an operand, so that it is the
+// compiler that writes m0 and knows it; the instruction wants a wait state behind that.
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
 // The same from base + offset of the lane, base in scalar registers: nothing to compute per lane and step.
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
 }
 // (As builtins and not in the asm, so that the compiler's own count of LDS reads in flight starts again from none.)
 template <int LATER>  // loads of this wavefront that may still be on their way, if some_later
