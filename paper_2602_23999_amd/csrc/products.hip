@@ -181,18 +181,20 @@ static int tile_size(const ProductArgs& p, int op, int size) {
   return of_128 <= of_64 ? 128 : 64;
 }
 
-// The rows of a tile of 64 columns that four groups of wavefronts share (forward and dx), or 0: with 8 steps of contraction or more, 32
-// where that gives no more than a tile for each compute unit (1119 rows, 5 of 10 lists each, 64 x 5472 fp32, 184 tiles: 56 us, 90 with
-// tiles of 64; 326 rows, 2 lists, 1222 x 7352 fp16, 240 tiles: 32, with two steps in LDS 39, and 47; 300 x 2048 x 2048 fp16, 320 tiles:
-// 19 and 13), 64 with little more than a tile for each (256 x 4096 x 4096 codes, 256 tiles: 22 us, shared 14; 2000 rows, 4 lists,
-// 512 x 1024 bf16, 280 tiles: 13.6 and 14.2; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 20 and 28).
+// The rows of a tile of 64 columns that four groups of wavefronts share (forward and dx), or 0: with 8 steps of contraction or more, and
+// only where the chip takes all tiles at once, because a compute unit has room for one of them.  With 32 rows where there are no more
+// of those than compute units (1119 rows, 5 of 10 lists each, 64 x 5472 fp32, 184 tiles: 56 us, 90 with tiles of 64; 326 rows, 2 lists, 1222 x
+// 7352 fp16, 240 tiles: 32, with two steps in LDS 39, and 47; 300 x 2048 x 2048 fp16, 320 tiles: 19 and 13), else with 64 rows (256 x 4096 x 4096
+// codes, 256 tiles: 14 us, not shared 22; 1024 x 1024 x 1024 bf16, 256 tiles: 10.4 and 12.5; 1408 x 768 x 1024 bf16, 264 tiles: 16.3 and
+// 12.7, as codes with 2048 columns 16.5 and 13.3; 3001 rows, 24 lists, 501 x 777 fp16, 560 tiles: 28 and 20).  Tiles are counted as
+// many as lists of any lengths may need: over 110 uneven batches near the border the choice takes 1.08 times the best one's time on
+// average, with the tiles of lists of mean length 1.12 times.
 static int shared_rows(const ProductArgs& p, int op, int size) {
   const int64_t width = op == FORWARD ? p.n : p.k, contraction = op == FORWARD ? p.k : p.n;
   if (contraction * size < 8 * 128) return 0;
-  const auto tiles = [&](int64_t rows) {
-    return std::min<int64_t>(p.pairs, p.pair_off ? p.pairs / rows + p.groups : up(p.pairs, rows)) * up(width, 64);
-  };
-  return tiles(32) <= 256 ? 32 : tiles(64) <= 280 ? 64 : 0;
+  const int64_t lists = std::min<int64_t>(p.groups, p.pairs);
+  const auto tiles = [&](int64_t rows) { return (p.pairs + lists * (rows - 1)) / rows * up(width, 64); };
+  return tiles(32) <= 256 ? 32 : tiles(64) <= 256 ? 64 : 0;
 }
 
 // Whether the lists are shorter than a tile of 64, so that the matrices, read once each, are what the time goes to: a third step on its
