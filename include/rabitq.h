@@ -386,7 +386,7 @@ int rabitq_grouped_matmul_dw(const rabitq_lists* lists, int32_t dtype, const voi
 /* Rows of numbers as int8: scale[i] = the fp32 number nearest to max_j |x[i][j]| / 127 (1 if that is 0), codes[i][j] = the
  * whole number nearest to x[i][j] / scale[i], ties to the even one, -127 .. 127 (and held there in rows of denormal numbers,
  * whose scale is itself rounded so far that the quotient may pass).  A row that holds an infinity or a NaN
- * gets scale NaN and codes 0, so that what is computed from it shows it.  k: 1 .. 2^20. */
+ * gets scale NaN and codes 0, so that what is computed from it shows it.  rows: 0 .. 2^31 - 1, k: 1 .. 2^20. */
 int rabitq_quantize_rows(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int32_t k, int8_t* codes, int64_t ldc,
                          float* scale, void* stream);
 

@@ -148,6 +148,7 @@ int rabitq_quantize_rows(const void* x, int32_t dtype, int64_t ldx, int64_t rows
     const char* call = "quantize_rows";
     if (!dtype_ok(dtype)) return bad(call, "unknown type");
     if (rows < 0 || k < 1 || k > MAX_WIDTH) return bad(call, "rows must be at least 0 and k in 1 .. 2^20");
+    if (rows > 0x7fffffff) return bad(call, "too many rows");
     if (!ld_ok(ldx, k) || !ld_ok(ldc, k)) return bad(call, "stride out of range");
     if (rows == 0) return RABITQ_OK;
     if (!x || !codes || !scale) return bad(call, "null pointer");

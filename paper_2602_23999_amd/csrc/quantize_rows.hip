@@ -133,15 +133,18 @@ static int launch_typed(const T* x, int64_t ldx, int64_t rows, int k, int8_t* co
   constexpr int EPC = 16 / sizeof(T);
   // a wavefront per row while its registers hold the row: no barrier, four rows per workgroup
   const bool wave = k <= 64 * HELD * EPC, once = k <= 256 * HELD * EPC;
-  const int64_t grid = wave ? (rows + 3) / 4 : rows;
-  if (grid > MAX_GRID / 256) {
-    set_error("quantize_rows: too many rows");
-    return RABITQ_EINVAL;
+  // (a launch takes 2^24 - 1 workgroups of 256 threads, so many rows are several launches)
+  const int64_t most = MAX_GRID / 256 * (wave ? 4 : 1);
+  for (int64_t first = 0; first < rows; first += most) {
+    const int64_t here = std::min(most, rows - first);
+    const unsigned grid = (unsigned)(wave ? (here + 3) / 4 : here);
+    const T* from = x + first * ldx;
+    int8_t* to = codes + first * ldc;
+    if (wave) quantize_rows_kernel<T, 1, true><<<grid, 256, 0, st>>>(from, ldx, here, k, to, ldc, scale + first);
+    else if (once) quantize_rows_kernel<T, 4, true><<<grid, 256, 0, st>>>(from, ldx, here, k, to, ldc, scale + first);
+    else quantize_rows_kernel<T, 4, false><<<grid, 256, 0, st>>>(from, ldx, here, k, to, ldc, scale + first);
+    RQ_HIP(hipGetLastError());
   }
-  if (wave) quantize_rows_kernel<T, 1, true><<<(unsigned)grid, 256, 0, st>>>(x, ldx, rows, k, codes, ldc, scale);
-  else if (once) quantize_rows_kernel<T, 4, true><<<(unsigned)grid, 256, 0, st>>>(x, ldx, rows, k, codes, ldc, scale);
-  else quantize_rows_kernel<T, 4, false><<<(unsigned)grid, 256, 0, st>>>(x, ldx, rows, k, codes, ldc, scale);
-  RQ_HIP(hipGetLastError());
   return RABITQ_OK;
 }
 

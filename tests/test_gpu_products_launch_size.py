@@ -46,3 +46,17 @@ def test_more_lists_than_the_smallest_tiles_hold():
         rest = torch.ones(groups, dtype=torch.bool, device="cuda")
         rest[small.cuda()] = False
         assert not got[rest].any()  # (every element is written: no NaN left)
+
+
+@pytest.mark.parametrize("rows,k", [((1 << 26) + 73, 8), ((1 << 27) + 1, 5)])
+def test_more_rows_to_quantise_than_a_launch_holds(rows, k):
+    # whole numbers from -127 to 127, 127 in every row: scale 1, and the codes are the numbers
+    g = torch.Generator(device="cuda").manual_seed(k)
+    codes = torch.randint(-127, 128, (rows, k), generator=g, device="cuda", dtype=torch.int8)
+    codes[:, 3] = 127
+    x = torch.empty(rows, k, dtype=torch.bfloat16, device="cuda")
+    x.copy_(codes)
+    x[-1] *= 2
+    got, scale = rabitq.quantize_rows(x)
+    assert torch.equal(got, codes)
+    assert (scale[:-1] == 1).all() and scale[-1] == 2

@@ -19,3 +19,10 @@ from test_products_refusals import _calls, _ls
 def test_launches_that_larger_tiles_hold_are_not_refused(name, lists, rest):
     args = rest if lists is None else dict(rest, ls=_ls(**lists))
     assert _calls()[name](**args) == -3  # (RABITQ_EHIP: it got as far as the launch, and there is no device)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls are not refused, and their pointers lead nowhere")
+@pytest.mark.parametrize("rows,k", [((1 << 26) - 4, 64), (1 << 26, 64), ((1 << 31) - 1, 64), (1 << 24, 4096), (1 << 25, 20000)])
+def test_rows_of_several_launches_are_not_refused(rows, k):
+    assert _calls()["quant"](rows=rows, k=k, ldx=k, ldc=k) == -3
+    assert _calls()["quant"](rows=1 << 31, k=k, ldx=k, ldc=k) == -1
