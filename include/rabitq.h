@@ -365,7 +365,7 @@ typedef struct {
  * stride_w elements from one matrix to the next (at least (n - 1) ldw + k), all of type `dtype`; one rounding, of the fp32 sum.
  * Rows of pairs that no list names are left as they were.
  * Errors (all calls of this section): RABITQ_EINVAL (null pointer, size or stride out of range, unknown type, more tiles of
- * work than one launch takes: 2^32 threads), RABITQ_EHIP. */
+ * work than one launch takes: about 2^24 of 128 rows of a list by 128 columns, those at an end counted whole), RABITQ_EHIP. */
 int rabitq_grouped_matmul(const rabitq_lists* lists, int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw,
                           int64_t stride_w, void* out, int64_t ldo, void* stream);
 

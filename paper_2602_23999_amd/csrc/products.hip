@@ -250,6 +250,9 @@ int launch_product_dx(const ProductArgs& p, int dtype, hipStream_t st) { return 
 // at least 512 positions, so that adding up costs less than it gains: 65 536 positions, 1 list, 512 x 512 bf16: 723 to 1449 us
 // without, 82 with parts of 2048; 20 000 positions, 256 x 256 fp32: 544 and 55.  Above the line parts lose:
 // 8192 positions, 4 lists, 2048 x 1024: 56 us without, 74 to 222 with; 3000, 24 lists, 512 x 768: 18 and 37.
+// This rule and the ones above know the mean length of the lists only, since the offsets lie in device memory.  It is dw that minds
+// uneven lists: 20 000 positions, 128 lists, 256 x 256, all lists alike: 18 us bf16, 41 fp32; nine positions of ten in one
+// list: 175 and 1246 (forward and dx: 21 and 42, 19 and 42).
 int dw_part(int64_t pairs, int groups, int64_t n, int64_t k) {
   const int64_t tiles = up(n, 128) * up(k, 128);
   if (tiles * groups >= 512) return 0;

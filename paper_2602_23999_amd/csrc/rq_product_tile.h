@@ -151,8 +151,7 @@ __global__ __launch_bounds__(64 * WI * WJ * KS) void product_tile_kernel(Product
   const int wi = wave / WJ, wj = wave % WJ;
 
   // which tile
-  const int nj = OP == FORWARD ? (int)0 : p.k;
-  const int64_t width = OP == FORWARD ? p.n : (int64_t)nj;  // of the output
+  const int64_t width = OP == FORWARD ? p.n : p.k;  // of the output
   const int64_t jt = (width + BJ - 1) / BJ;
   // Workgroups go to the 8 XCDs in turn.  An XCD gets strips of up to 8 neighbouring columns of tiles, whose share of a comes to its L2
   // once.  (Strips of one row of tiles: 64 lists of 512 rows, 2048 x 2048 codes: 179 us; blocks of 4 x 8 tiles, which read
